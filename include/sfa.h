@@ -497,6 +497,233 @@ sfa_status sfa_attn_decode_q8(const float* q, const void* q_idx, const void* q_v
                               int q_val_t, int kc_idx_t, int o_t, void* o, float* lse, void* ws,
                               size_t ws_bytes, void* stream);
 
+/*
+ * Rotary positions with several axes.
+ *
+ * A plan says which coordinates of a d-dimensional head are turned and how:
+ * pair i (0 <= i < rot/2, rot = 2 * (sum of sections)) is the coordinates
+ * (i, i + rot/2) or (2i, 2i + 1) and turns by pos[axis[i]] * freq[i] radians;
+ * coordinates from rot on are copied.  Text has one axis; video three (time,
+ * height, width), section a being the pairs of axis a.
+ *   SFA_ROPE_SECTIONS     axis 0 has the first sections[0] pairs, axis 1 the
+ *                         next, ...; freq[i] = theta^(-2i / rot)
+ *   SFA_ROPE_INTERLEAVED  the pairs are dealt to the axes in turn, an axis
+ *                         dropping out once it has its section's count;
+ *                         freq[i] as above
+ *   SFA_ROPE_OWN          consecutive runs as in SECTIONS, each axis with its
+ *                         own ladder: its j-th pair has theta^(-j / sections[a])
+ * The plan is a plain struct that the caller owns; the calls below copy what
+ * they need from it, and it may be freed or changed as soon as they return.
+ */
+#define SFA_ROPE_MAX_AXES 4
+#define SFA_ROPE_MAX_PAIRS 128
+typedef enum { SFA_ROPE_HALVES = 0, SFA_ROPE_NEIGHBOURS = 1 } sfa_rope_pairing;
+typedef enum { SFA_ROPE_SECTIONS = 0, SFA_ROPE_INTERLEAVED = 1, SFA_ROPE_OWN = 2 } sfa_rope_order;
+typedef struct {
+  int32_t d, rot, naxes, pairing;
+  double freq[SFA_ROPE_MAX_PAIRS];  /* radians per position */
+  uint8_t axis[SFA_ROPE_MAX_PAIRS];
+} sfa_rope_plan;
+
+/*
+ * Fills a plan (host only; no GPU work).
+ * Limits: 1 <= naxes <= 4, every section >= 1, 2 * sum <= d <= 256 (SFA_ENOTSUP
+ * above 256), theta finite and >= 1.
+ * Errors: SFA_EINVAL, SFA_ENOTSUP.
+ */
+sfa_status sfa_rope_plan_init(sfa_rope_plan* plan, int d, const int32_t* sections, int naxes,
+                              double theta, int pairing, int order);
+
+/*
+ * y = R(pos) x, or R(pos)^T x with `inverse` (the gradient of the rotation:
+ * dx = R^T dy).  For the pair (x1, x2) with angle a:
+ *   y1 = x1 cos a - x2 sin a,   y2 = x2 cos a + x1 sin a.
+ * The angle and its sine and cosine are taken in float64 (positions of any
+ * int32 value keep their phase); cosine and sine are rounded to float32, the
+ * products are exact in float64, and each y is rounded to float32 once (and
+ * then, for SFA_BF16, to nearest-even bfloat16).
+ *
+ * x        [B, H, n, d] of x_t (SFA_F32 or SFA_BF16), coordinates contiguous,
+ *          element strides x_strides = {batch, head, token} (>= 0), or NULL
+ *          for a contiguous array: a view of a packed projection needs no copy.
+ * pos      [naxes, B, n] int32, tokens contiguous; element strides
+ *          pos_axis_stride and pos_batch_stride (0: shared by all axes / by all
+ *          sequences).
+ * y        like x, of y_t, with y_strides (each dimension of more than one
+ *          entry has a stride of at least d: rows do not overlap).  y may be x
+ *          itself, with the same strides and type; any other overlap is
+ *          undefined.
+ * Limits: B, H >= 1, n >= 0 (0 is a no-op); B * n and H <= 2^31 - 1.
+ * Errors: SFA_EINVAL, SFA_EHIP.
+ */
+sfa_status sfa_rope(const void* x, const int64_t* x_strides, const int32_t* pos,
+                    int64_t pos_axis_stride, int64_t pos_batch_stride, const sfa_rope_plan* plan,
+                    int B, int H, int n, int inverse, int x_t, int y_t, void* y,
+                    const int64_t* y_strides, void* stream);
+
+/*
+ * Rotation and Top-k coding in one pass: the code of y = R(pos) x (y in
+ * float32, as sfa_rope writes it) exactly as sfa_topk_encode codes it, without
+ * y going through memory.
+ * x, x_strides, x_t, pos, plan: as sfa_rope.
+ * idx, val [B, H, n, k] contiguous, of idx_t / val_t: as sfa_topk_encode.
+ * Limits: as sfa_rope; 1 <= k <= d.
+ * Errors: SFA_EINVAL, SFA_EHIP.
+ */
+sfa_status sfa_rope_encode(const void* x, const int64_t* x_strides, const int32_t* pos,
+                           int64_t pos_axis_stride, int64_t pos_batch_stride,
+                           const sfa_rope_plan* plan, int B, int H, int n, int k, int x_t,
+                           void* idx, int idx_t, void* val, int val_t, void* stream);
+
+/*
+ * Backward of sfa_rope_encode with the straight-through estimator (Sec. 3.1,
+ * Eq. (6): the gradient of a coordinate is that of its code value on the
+ * support and 0 elsewhere):  dx = R(pos)^T scatter(idx, dval).
+ * idx, dval [B, H, n, k] contiguous: the code's indices (idx_t) and the float32
+ *           gradients of its values, as sfa_attn_bwd returns them.  Indices are
+ *           distinct within a row; they are masked into range before use.
+ * dx        [B, H, n, d] of dx_t (SFA_F32 or SFA_BF16), dx_strides as y_strides
+ *           of sfa_rope; every coordinate is written.
+ * Limits: as sfa_rope_encode.
+ * Errors: SFA_EINVAL, SFA_EHIP.
+ */
+sfa_status sfa_rope_encode_bwd(const void* idx, int idx_t, const float* dval, const int32_t* pos,
+                               int64_t pos_axis_stride, int64_t pos_batch_stride,
+                               const sfa_rope_plan* plan, int B, int H, int n, int k, int dx_t,
+                               void* dx, const int64_t* dx_strides, void* stream);
+
+/*
+ * Block tables and slot maps on the device, from request lengths.
+ *
+ * Each sequence b goes from old_len[b] to new_len[b] cached positions.  One that
+ * grows takes pages for the positions that its pages do not reach; one that
+ * shrinks (a rejected draft; new_len 0: a request that ended) gives back the
+ * pages past its new end.  Pages are given back first and may be taken again in
+ * the same call.
+ *
+ * old_len, new_len [B] int32 (clamped into [0, max_pages * page_size]); old_len
+ *             NULL: every sequence starts empty.
+ * block_table [B, max_pages] int32 in/out: the first ceil(old / page_size) entries
+ *             of a row are its pages.  Entries of new pages are written, all
+ *             others left as they were (those of a page given back included).
+ * free_pages  [num_pages] int32 in/out and free_in [1]: the free list, a stack
+ *             whose first free_in[0] entries (clamped into [0, num_pages]) are
+ *             free page ids.  Pages given back are pushed in order of sequence
+ *             and page, then new pages are popped from the top in order of
+ *             sequence and page.  Only entries that are pushed and not popped are
+ *             written.
+ * free_out    [1] int32: the new count of free pages.  May be free_in itself.
+ * got_len     [B] int32: new_len, or as far as the free pages reached (a sequence
+ *             that found none keeps old_len, or the end of its last page).  May
+ *             not be old_len or new_len.
+ * starts      [B + 1] int32 or NULL: sequence b's new tokens are rows starts[b] ..
+ *             starts[b + 1] - 1 of a packed token buffer; max(0, new - old) each, as
+ *             requested, got or not (the total must be below 2^31).
+ * slots       [n_rows] int32 or NULL: the cache slot page * page_size + offset of
+ *             each row's token, for sfa_kv_append_q4; -1 for a token past got_len,
+ *             for one whose page id is outside [0, num_pages), and for the rows
+ *             behind the last token.  Tokens past n_rows have no row.
+ * positions   [n_rows] int32 or NULL: each row's position in its sequence (as
+ *             sfa_rope takes it), -1 behind the last token.
+ * ws          caller-owned device workspace of sfa_page_tables_workspace(B) bytes;
+ *             needs no initialisation, scratch after the call.
+ * With free_out other than free_in the call may be repeated with the same result.
+ * Limits: 1 <= B <= 2^20; max_pages >= 1; page_size a power of two; num_pages >= 1;
+ *         max_pages * page_size <= 2^30; num_pages * page_size < 2^31;
+ *         B * max_pages < 2^31; n_rows >= 0.
+ * Errors: SFA_EINVAL, SFA_ENOSPC, SFA_EHIP.
+ */
+sfa_status sfa_page_tables(const int32_t* old_len, const int32_t* new_len, int B,
+                           int32_t* block_table, int max_pages, int page_size,
+                           int32_t* free_pages, int num_pages, const int32_t* free_in,
+                           int32_t* free_out, int32_t* got_len, int32_t* starts, int32_t* slots,
+                           int32_t* positions, int n_rows, void* ws, size_t ws_bytes,
+                           void* stream);
+
+/* Bytes of device workspace sfa_page_tables needs (0 for an invalid B). */
+size_t sfa_page_tables_workspace(int B);
+
+/*
+ * 4-bit KV cache: the 8-bit cache above with signed 4-bit numbers,
+ *     q = round-half-even(x / s) in [-7, 7]
+ * (the float32 division correctly rounded; s = 0: q = 0).  A key's k code values
+ * share s = max |x| / 7 in float32.  A value row has one s for each run of 32
+ * coordinates, s = max |v| / 7 rounded to nearest-even bfloat16: a row's outlying
+ * coordinates then cost only their own run.  The cache stands for q * s.
+ *
+ * Layout (rows as for the 8-bit cache; two numbers to a byte in two's complement,
+ * the lower coordinate in the low half):
+ *     kc_idx   [rows, k] uint8        kc_val  [rows, k / 2] bytes
+ *     kc_scale [rows] float32         v_cache [rows, d / 2] bytes
+ *     v_scale  [rows, d / 32] bfloat16
+ * 100 bytes per cached key and KV head at d = 128, k = 16, against 184 in the 8-bit
+ * cache and 320 with int16 / bf16 codes and bf16 V.
+ */
+
+/*
+ * Append to a 4-bit cache.
+ *
+ * k_new, v_new [B, Hkv, T, d] of k_new_t / v_new_t (SFA_F32 or SFA_BF16), element
+ *          strides kv_strides = {k batch, head, token, v batch, head, token} (>= 0),
+ *          or NULL for contiguous arrays.  A packed buffer of ragged sequences
+ *          [tokens, Hkv, d] is B = 1, T = tokens.
+ * Where the tokens go, one of:
+ *   slots  [B, T] int32: token (b, t) of every head goes to slot
+ *          page * page_size + offset (sfa_page_tables writes such maps), in the
+ *          contiguous cache b' * page_size + position; slots outside
+ *          [0, num_pages * page_size) are not written.  Slots are distinct.
+ *          seq_len, n_new and block_table are NULL.
+ *   seq_len (and n_new, block_table): as sfa_kv_append, seq_len advanced.
+ * num_pages  pages of the pool; with a contiguous cache (block_table NULL) the B
+ *          sequences of page_size = Lmax positions.
+ * k_idx, k_val, v_out: NULL, or what the cache now stands for, as a prompt's
+ *          forward reads it (so that it attends over the same numbers as the decode
+ *          that follows): codes [B, Hkv, T, k], int16 and float32 q * s, and values
+ *          [B, Hkv, T, d], bfloat16 (q * s rounded to nearest even).  k_idx and
+ *          k_val go together.  Rows of tokens that are not written to the cache are
+ *          left as they were.
+ * Limits: d a multiple of 32, k a multiple of 8, k <= d <= 256 (SFA_ENOTSUP
+ *         otherwise); B * Hkv * T <= 2^31; num_pages * page_size < 2^31;
+ *         page_size a power of two with block_table (any with slots or a
+ *         contiguous cache).
+ * Errors: SFA_EINVAL, SFA_ENOTSUP, SFA_EHIP.
+ */
+sfa_status sfa_kv_append_q4(const void* k_new, const void* v_new, const int64_t* kv_strides,
+                            const int32_t* slots, const int32_t* n_new, int32_t* seq_len, int B,
+                            int Hkv, int T, int d, int k, const int32_t* block_table,
+                            int max_pages, int page_size, int num_pages, uint8_t* kc_idx,
+                            uint8_t* kc_val, float* kc_scale, uint8_t* v_cache, uint16_t* v_scale,
+                            int16_t* k_idx, float* k_val, uint16_t* v_out, int k_new_t,
+                            int v_new_t, void* stream);
+
+/*
+ * Decode step over a 4-bit cache: sfa_attn_decode_q8 with key j's code values
+ * q_ju * ks_j and value coordinates q_jc * vs_j,c/32.  Scores and softmax in float32;
+ * in P.V each weight p_j * vs_j,c/32 enters the matrix cores as two float16 pieces
+ * (relative 2^-22; as a whole scaled by a power of two, so that scales of any
+ * magnitude keep it) against the exact integers q, with float32 accumulation.
+ * q / q_idx, q_val, block_table, seq_len, window, n_global, o, lse: as
+ * sfa_attn_decode_q8; a sequence with 0 keys gets O = 0 and LSE = -inf.
+ * ws: sfa_attn_decode_q4_workspace(B, Hq, capacity, d) bytes, scratch.
+ * Limits: d a multiple of 32, k a multiple of 8, k <= d <= 256, Hq / Hkv <= 8 (any
+ *         group; SFA_ENOTSUP otherwise); cache arrays 16-byte aligned (the scales 4
+ *         and 2); paged: page_size a power of two >= 16; capacity <= 2^30;
+ *         B * Hkv <= 65535.
+ * Errors: SFA_EINVAL, SFA_ENOTSUP, SFA_ENOSPC, SFA_EHIP.
+ */
+sfa_status sfa_attn_decode_q4(const float* q, const void* q_idx, const void* q_val,
+                              const uint8_t* kc_idx, const uint8_t* kc_val,
+                              const float* kc_scale, const uint8_t* v_cache,
+                              const uint16_t* v_scale, const int32_t* block_table, int max_pages,
+                              int page_size, int num_pages, const int32_t* seq_len, int B, int Hq,
+                              int Hkv, int d, int k, float scale, int window, int n_global,
+                              int q_idx_t, int q_val_t, int o_t, void* o, float* lse, void* ws,
+                              size_t ws_bytes, void* stream);
+
+/* Bytes of device workspace sfa_attn_decode_q4 needs, for any Hkv and window (0 for
+ * invalid sizes). */
+size_t sfa_attn_decode_q4_workspace(int B, int Hq, int Lmax, int d);
+
 #ifdef __cplusplus
 }
 #endif

@@ -11,3 +11,6 @@ from .sfa_oracle import (  # noqa: F401
     f16_rne, widen_f16, topk_encode_f16, csr_densify, csr_to_fixed, token_mask,
     quant_q8, dequant_q8, kv_append_q8, stored_output,
 )
+from .sfa_operators import (  # noqa: F401
+    rope, rope_ladder, rope_pairs, page_tables, quant_q4, pack_q4, unpack_q4, rows_q4, values_q4,
+)

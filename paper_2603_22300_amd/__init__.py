@@ -20,7 +20,9 @@ __all__ = [
     "sfa_attn_bwd_workspace", "sfa_attn_bwd",
     "sfa_attn_decode_workspace", "sfa_attn_decode", "sfa_attn_decode_noalloc",
     "sfa_attn_decode_paged", "sfa_kv_append", "sfa_kv_append_q8", "sfa_attn_decode_q8",
-    "sfa_csr_to_codes",
+    "sfa_csr_to_codes", "RopePlan", "sfa_rope_plan", "sfa_rope", "sfa_rope_encode",
+    "sfa_rope_encode_bwd", "sfa_page_tables", "sfa_page_tables_workspace", "sfa_kv_append_q4",
+    "sfa_attn_decode_q4", "sfa_attn_decode_q4_workspace",
     "SFA_OK", "SFA_EINVAL", "SFA_ENOTSUP", "SFA_EHIP", "SFA_ENOSPC",
     "SFA_I32", "SFA_I16", "SFA_F32", "SFA_BF16", "SFA_U8", "SFA_F16",
 ]
@@ -32,6 +34,15 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 library_path = os.path.join(_HERE, "libsfa.so")
 
 _lib = None
+
+
+_ROPE_MAX_PAIRS = 128
+
+
+class _RopePlan(ctypes.Structure):  # sfa_rope_plan
+    _fields_ = [("d", ctypes.c_int32), ("rot", ctypes.c_int32), ("naxes", ctypes.c_int32),
+                ("pairing", ctypes.c_int32), ("freq", ctypes.c_double * _ROPE_MAX_PAIRS),
+                ("axis", ctypes.c_uint8 * _ROPE_MAX_PAIRS)]
 
 
 class SfaError(RuntimeError):
@@ -93,6 +104,33 @@ def lib() -> ctypes.CDLL:
                                          i32, vp, vp, vp, sz, vp]
         L.sfa_csr_to_codes.restype = i32
         L.sfa_csr_to_codes.argtypes = [vp, vp, i32, vp, i32, i64, i32, i32, vp, i32, vp, vp]
+        strides, plan = ctypes.POINTER(i64), ctypes.POINTER(_RopePlan)
+        L.sfa_rope_plan_init.restype = i32
+        L.sfa_rope_plan_init.argtypes = [plan, i32, ctypes.POINTER(ctypes.c_int32), i32,
+                                         ctypes.c_double, i32, i32]
+        L.sfa_rope.restype = i32
+        L.sfa_rope.argtypes = [vp, strides, vp, i64, i64, plan, i32, i32, i32, i32, i32, i32, vp,
+                               strides, vp]
+        L.sfa_rope_encode.restype = i32
+        L.sfa_rope_encode.argtypes = [vp, strides, vp, i64, i64, plan, i32, i32, i32, i32, i32, vp,
+                                      i32, vp, i32, vp]
+        L.sfa_rope_encode_bwd.restype = i32
+        L.sfa_rope_encode_bwd.argtypes = [vp, i32, vp, vp, i64, i64, plan, i32, i32, i32, i32, i32,
+                                          vp, strides, vp]
+        L.sfa_page_tables_workspace.restype = sz
+        L.sfa_page_tables_workspace.argtypes = [i32]
+        L.sfa_page_tables.restype = i32
+        L.sfa_page_tables.argtypes = [vp, vp, i32, vp, i32, i32, vp, i32, vp, vp, vp, vp, vp, vp,
+                                      i32, vp, sz, vp]
+        L.sfa_kv_append_q4.restype = i32
+        L.sfa_kv_append_q4.argtypes = [vp, vp, strides, vp, vp, vp, i32, i32, i32, i32, i32, vp,
+                                       i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, i32, i32, vp]
+        L.sfa_attn_decode_q4_workspace.restype = sz
+        L.sfa_attn_decode_q4_workspace.argtypes = [i32, i32, i32, i32]
+        L.sfa_attn_decode_q4.restype = i32
+        L.sfa_attn_decode_q4.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, vp,
+                                         i32, i32, i32, i32, i32, f32, i32, i32, i32, i32, i32, vp,
+                                         vp, vp, sz, vp]
         _lib = L
     return _lib
 
@@ -581,3 +619,356 @@ def sfa_csr_to_codes(indptr, indices, values, d: int, kmax: int, idx_dtype=None,
                                  vit, rows, d, kmax, idx.data_ptr(), it, val.data_ptr(),
                                  _stream(indptr)), "sfa_csr_to_codes")
     return idx, val
+
+
+# ---------------------------------------------------------------------------
+# Rotary positions
+# ---------------------------------------------------------------------------
+
+_PAIRINGS = {"halves": 0, "neighbours": 1}
+_ORDERS = {"sections": 0, "interleaved": 1, "own": 2}
+
+
+def _launch(t: torch.Tensor, name: str, *args):
+    """The C call on torch's current stream of t's device, with that device current."""
+    dev = t.device.index
+    fn = getattr(lib(), name)
+    if torch.cuda.current_device() == dev:
+        _call(fn(*args, _stream(t)), name)
+    else:
+        with torch.cuda.device(dev):
+            _call(fn(*args, _stream(t)), name)
+
+
+def _together(t: torch.Tensor, **others):
+    for name, u in others.items():
+        if u is not None and u.device != t.device:
+            raise ValueError(f"{name} is on {u.device}, not on {t.device}")
+
+
+def _rows4(t: torch.Tensor, name: str, table):
+    """Checks a [B, H, n, d] tensor whose coordinates are contiguous (any strides else);
+    returns its dtype code and a C array of its batch, head and token strides."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a GPU tensor (got {t.device})")
+    code = table.get(t.dtype)
+    if code is None:
+        raise TypeError(f"{name}: unsupported dtype {t.dtype}")
+    if t.dim() != 4:
+        raise ValueError(f"{name} must be [B, H, n, d]")
+    st = t.stride()
+    if st[3] != 1 and t.shape[3] != 1:
+        raise ValueError(f"{name}: a row's coordinates must be contiguous")
+    return code, (ctypes.c_int64 * 3)(*st[:3])
+
+
+class RopePlan:
+    """Which coordinates of a head turn, by which axis' position and how fast: the
+    caller's handle for the sfa_rope* calls (host data only, no GPU memory)."""
+
+    def __init__(self, d, sections, theta, pairing, order):
+        self._c = _RopePlan()
+        sec = (ctypes.c_int32 * max(1, len(sections)))(*sections)
+        _call(lib().sfa_rope_plan_init(ctypes.byref(self._c), d, sec, len(sections), float(theta),
+                                       pairing, order), "sfa_rope_plan_init")
+        self.ref = ctypes.byref(self._c)
+
+    d = property(lambda self: self._c.d)
+    rot = property(lambda self: self._c.rot)
+    naxes = property(lambda self: self._c.naxes)
+    freq = property(lambda self: list(self._c.freq)[:self._c.rot // 2])
+    axis = property(lambda self: list(self._c.axis)[:self._c.rot // 2])
+
+
+def sfa_rope_plan(d: int, sections=None, theta: float = 10000.0, pairing: str = "halves",
+                  order: str = "sections") -> RopePlan:
+    """Plan of rotary positions for heads of d coordinates.  sections: pairs per
+    axis (None: one axis over all d // 2 pairs); the first 2 * sum(sections)
+    coordinates turn, the rest are copied.  pairing: pair i is coordinates "halves"
+    (i, i + rot / 2) or "neighbours" (2 i, 2 i + 1).  order: "sections" (runs of
+    pairs on one frequency ladder), "interleaved" (pairs dealt to the axes in turn)
+    or "own" (runs of pairs, each axis its own ladder)."""
+    if pairing not in _PAIRINGS:
+        raise ValueError(f"pairing must be one of {sorted(_PAIRINGS)}")
+    if order not in _ORDERS:
+        raise ValueError(f"order must be one of {sorted(_ORDERS)}")
+    return RopePlan(d, list(sections) if sections is not None else [d // 2], theta,
+                    _PAIRINGS[pairing], _ORDERS[order])
+
+
+def _pos(pos, plan, t, B, n):
+    """Position tensor [naxes, B, n], [B, n] or [n] (int32, tokens contiguous; entries of
+    size 1 are shared): its address and its axis and batch strides."""
+    if not isinstance(pos, torch.Tensor) or pos.dtype != torch.int32:
+        raise TypeError("pos must be an int32 tensor")
+    if not isinstance(plan, RopePlan):
+        raise TypeError("plan must come from sfa_rope_plan")
+    _together(t, pos=pos)
+    shape = (1,) * (3 - pos.dim()) + tuple(pos.shape)
+    st = (0,) * (3 - pos.dim()) + tuple(pos.stride())
+    if len(shape) != 3 or shape[0] not in (1, plan.naxes) or shape[1] not in (1, B) or shape[2] != n:
+        raise ValueError("pos must be [naxes, B, n], [B, n] or [n]")
+    if n > 1 and st[2] != 1:
+        raise ValueError("pos: tokens must be contiguous")
+    return pos.data_ptr(), st[0] if shape[0] > 1 else 0, st[1] if shape[1] > 1 else 0
+
+
+def sfa_rope(x, pos, plan: RopePlan, inverse: bool = False, y_dtype=None,
+             y: torch.Tensor | None = None):
+    """Rotary positions on x [B, H, n, d] (float32 or bf16; any strides with
+    contiguous coordinates): y of y_dtype (default x's), or into the caller's y
+    (which may be x).  inverse=True turns back: the gradient of the rotation."""
+    xt, xs = _rows4(x, "x", _VAL)
+    B, H, n, d = x.shape
+    if d != plan.d:
+        raise ValueError(f"x has {d} coordinates, the plan {plan.d}")
+    pp, pa, pb = _pos(pos, plan, x, B, n)
+    if y is None:
+        y = torch.empty((B, H, n, d), dtype=y_dtype or x.dtype, device=x.device)
+    yt, ys = _rows4(y, "y", _VAL)
+    _together(x, y=y)
+    if tuple(y.shape) != (B, H, n, d):
+        raise ValueError("y has the wrong shape")
+    if B and H and n:
+        _launch(x, "sfa_rope", x.data_ptr(), xs, pp, pa, pb, plan.ref, B, H, n, int(bool(inverse)),
+                xt, yt, y.data_ptr(), ys)
+    return y
+
+
+def sfa_rope_encode(x, pos, plan: RopePlan, k: int, idx_dtype=torch.int32, val_dtype=torch.float32,
+                    idx: torch.Tensor | None = None, val: torch.Tensor | None = None):
+    """Top-k codes of the rotated rows of x [B, H, n, d] in one pass: (idx, val)
+    [B, H, n, k], as sfa_topk_encode of sfa_rope's float32 rows."""
+    xt, xs = _rows4(x, "x", _VAL)
+    B, H, n, d = x.shape
+    if d != plan.d:
+        raise ValueError(f"x has {d} coordinates, the plan {plan.d}")
+    pp, pa, pb = _pos(pos, plan, x, B, n)
+    if idx is None:
+        idx = torch.empty((B, H, n, k), dtype=idx_dtype, device=x.device)
+    if val is None:
+        val = torch.empty((B, H, n, k), dtype=val_dtype, device=x.device)
+    it, vt = _check(idx, "idx", _IDX), _check(val, "val", _CVAL)
+    _together(x, idx=idx, val=val)
+    if tuple(idx.shape) != (B, H, n, k) or tuple(val.shape) != (B, H, n, k):
+        raise ValueError("idx and val must be [B, H, n, k]")
+    if B and H and n:
+        _launch(x, "sfa_rope_encode", x.data_ptr(), xs, pp, pa, pb, plan.ref, B, H, n, k, xt,
+                idx.data_ptr(), it, val.data_ptr(), vt)
+    return idx, val
+
+
+def sfa_rope_encode_bwd(idx, dval, pos, plan: RopePlan, dx_dtype=torch.float32,
+                        dx: torch.Tensor | None = None):
+    """Backward of sfa_rope_encode (straight-through): the gradients dval [B, H, n, k]
+    float32 of the code values, at idx [B, H, n, k], turned back into dx [B, H, n, d]
+    (dx_dtype, or the caller's dx: float32 or bf16, any strides with contiguous
+    coordinates, every coordinate written)."""
+    it = _check(idx, "idx", _IDX)
+    _check(dval, "dval", _F32)
+    if idx.dim() != 4 or tuple(dval.shape) != tuple(idx.shape):
+        raise ValueError("idx and dval must be [B, H, n, k]")
+    B, H, n, k = idx.shape
+    pp, pa, pb = _pos(pos, plan, idx, B, n)
+    if dx is None:
+        dx = torch.empty((B, H, n, plan.d), dtype=dx_dtype, device=idx.device)
+    xt, xs = _rows4(dx, "dx", _VAL)
+    _together(idx, dval=dval, dx=dx)
+    if tuple(dx.shape) != (B, H, n, plan.d):
+        raise ValueError("dx has the wrong shape")
+    if B and H and n:
+        _launch(idx, "sfa_rope_encode_bwd", idx.data_ptr(), it, dval.data_ptr(), pp, pa, pb,
+                plan.ref, B, H, n, k, xt, dx.data_ptr(), xs)
+    return dx
+
+
+# ---------------------------------------------------------------------------
+# Block tables and slot maps
+# ---------------------------------------------------------------------------
+
+
+def sfa_page_tables_workspace(B: int) -> int:
+    """Bytes of device workspace sfa_page_tables needs."""
+    return int(lib().sfa_page_tables_workspace(B))
+
+
+def sfa_page_tables(old_len, new_len, block_table, free_pages, free_in, page_size: int,
+                    free_out=None, got=None, starts=None, slots=None, pos=None, n_rows: int = 0,
+                    ws=None):
+    """Takes every sequence from old_len to new_len cached positions (int32 [B];
+    old_len None: all empty): pages are given back to and taken from the free list,
+    block_table [B, max_pages] and free_pages [num_pages] (a stack whose first
+    free_in[0] entries are free) are updated in place, and the new tokens of a packed
+    buffer get their slots and positions.  slots and pos (int32 [n_rows]) are
+    allocated when n_rows > 0 and none are given.  free_out may be free_in.
+    Returns (got, free_out, starts, slots, pos): the lengths that the pages reached
+    [B], the new free count [1], the first row of each sequence [B + 1], and the maps
+    (or None)."""
+    _check(new_len, "new_len", _I32)
+    B = new_len.numel()
+    op = _i32_vec(old_len, "old_len", B) if old_len is not None else 0
+    _check(block_table, "block_table", _I32)
+    if block_table.dim() != 2 or block_table.shape[0] != B:
+        raise ValueError("block_table must be [B, max_pages]")
+    _check(free_pages, "free_pages", _I32)
+    new = dict(dtype=torch.int32, device=new_len.device)
+    free_out = torch.empty((1,), **new) if free_out is None else free_out
+    got = torch.empty((B,), **new) if got is None else got
+    starts = torch.empty((B + 1,), **new) if starts is None else starts
+    if slots is None and pos is None and n_rows > 0:
+        slots, pos = torch.empty((n_rows,), **new), torch.empty((n_rows,), **new)
+    rows = slots.numel() if slots is not None else pos.numel() if pos is not None else 0
+    sp = _i32_vec(slots, "slots", rows) if slots is not None else 0
+    pp = _i32_vec(pos, "pos", rows) if pos is not None else 0
+    if ws is None:
+        ws = torch.empty(sfa_page_tables_workspace(B), dtype=torch.uint8, device=new_len.device)
+    if ws.device != new_len.device or not ws.is_contiguous():
+        raise ValueError("ws must be a contiguous tensor on the same GPU")
+    _together(new_len, old_len=old_len, block_table=block_table, free_pages=free_pages,
+              free_in=free_in, free_out=free_out, got=got, starts=starts, slots=slots, pos=pos)
+    _launch(new_len, "sfa_page_tables", op, new_len.data_ptr(), B, block_table.data_ptr(),
+            block_table.shape[1], page_size, free_pages.data_ptr(), free_pages.numel(),
+            _i32_vec(free_in, "free_in", 1), _i32_vec(free_out, "free_out", 1),
+            _i32_vec(got, "got", B), _i32_vec(starts, "starts", B + 1), sp, pp, rows,
+            ws.data_ptr(), ws.numel() * ws.element_size())
+    return got, free_out, starts, slots, pos
+
+
+# ---------------------------------------------------------------------------
+# 4-bit cache
+# ---------------------------------------------------------------------------
+
+_U8, _I16, _BF16 = {torch.uint8: 0}, {torch.int16: 0}, {torch.bfloat16: SFA_BF16}
+
+
+def _q4_cache(kc_idx, kc_val, kc_scale, v_cache, v_scale):
+    """Checks the five arrays of a 4-bit cache; returns (pages, Hkv, page_size, k, d)."""
+    _check(kc_idx, "kc_idx", _U8); _check(kc_val, "kc_val", _U8); _check(kc_scale, "kc_scale", _F32)
+    _check(v_cache, "v_cache", _U8); _check(v_scale, "v_scale", _BF16)
+    if kc_idx.dim() != 4:
+        raise ValueError("kc_idx must be [pages, Hkv, page_size, k]")
+    rows, k, d = tuple(kc_idx.shape[:3]), kc_idx.shape[3], 2 * v_cache.shape[-1]
+    if tuple(kc_val.shape) != rows + (k // 2,) or tuple(kc_scale.shape) != rows \
+            or tuple(v_cache.shape) != rows + (d // 2,) or tuple(v_scale.shape) != rows + (d // 32,):
+        raise ValueError("inconsistent cache shapes")
+    _together(kc_idx, kc_val=kc_val, kc_scale=kc_scale, v_cache=v_cache, v_scale=v_scale)
+    return rows + (k, d)
+
+
+def sfa_kv_append_q4(k_new, v_new, seq_len, kc_idx, kc_val, kc_scale, v_cache, v_scale, k: int,
+                     block_table=None, n_new=None, slots=None, k_idx=None, k_val=None, v_out=None):
+    """Append to a 4-bit cache: kc_idx uint8 [.., k], kc_val uint8 [.., k/2] (two signed
+    4-bit numbers a byte), kc_scale float32, v_cache uint8 [.., d/2], v_scale bf16
+    [.., d/32], each over [pages, Hkv, page_size] rows (contiguous: [B, Hkv, Lmax]).
+    k_new, v_new [B, Hkv, T, d] float32 or bf16, any strides with contiguous
+    coordinates (a packed [tokens, Hkv, d] buffer is a view with B = 1).  Either seq_len
+    (int32 [B], advanced in place), with n_new and block_table as sfa_kv_append, or
+    seq_len None and slots [B, T] int32 (as sfa_page_tables writes them; rows outside
+    the pool are skipped).  k_idx int16 and k_val float32 [B, Hkv, T, k], v_out bf16
+    [B, Hkv, T, d]: if given, the numbers the cache now stands for."""
+    kt, kst = _rows4(k_new, "k_new", _VAL)
+    vt, vst = _rows4(v_new, "v_new", _VAL)
+    B, Hkv, T, d = k_new.shape
+    if tuple(v_new.shape) != (B, Hkv, T, d):
+        raise ValueError("v_new must match k_new")
+    pages, hkv, P, kc, dc = _q4_cache(kc_idx, kc_val, kc_scale, v_cache, v_scale)
+    if (hkv, kc, dc) != (Hkv, k, d):
+        raise ValueError("inconsistent cache shapes")
+    sp = lp = np_ = tp = maxp = 0
+    if slots is not None:
+        if seq_len is not None or n_new is not None or block_table is not None:
+            raise ValueError("slots say where every token goes: give no seq_len, n_new or block_table")
+        sp = _i32_vec(slots, "slots", B * T)
+    else:
+        lp = _i32_vec(seq_len, "seq_len", B)
+        np_ = _i32_vec(n_new, "n_new", B) if n_new is not None else 0
+        if block_table is not None:
+            _check(block_table, "block_table", _I32)
+            if block_table.dim() != 2 or block_table.shape[0] != B:
+                raise ValueError("block_table must be [B, max_pages]")
+            tp, maxp = block_table.data_ptr(), block_table.shape[1]
+        elif pages != B:
+            raise ValueError("a contiguous cache holds B sequences")
+    outs = [0, 0, 0]
+    for i, (t, name, table, shape) in enumerate(((k_idx, "k_idx", _I16, (B, Hkv, T, k)),
+                                                 (k_val, "k_val", _F32, (B, Hkv, T, k)),
+                                                 (v_out, "v_out", _BF16, (B, Hkv, T, d)))):
+        if t is not None:
+            _check(t, name, table)
+            if tuple(t.shape) != shape:
+                raise ValueError(f"{name} has the wrong shape")
+            outs[i] = t.data_ptr()
+    _together(k_new, v_new=v_new, kc_idx=kc_idx, seq_len=seq_len, n_new=n_new,
+              block_table=block_table, slots=slots, k_idx=k_idx, k_val=k_val, v_out=v_out)
+    st = (ctypes.c_int64 * 6)(*kst, *vst)
+    _launch(k_new, "sfa_kv_append_q4", k_new.data_ptr(), v_new.data_ptr(), st, sp, np_, lp, B, Hkv,
+            T, d, k, tp, maxp, P, pages, kc_idx.data_ptr(), kc_val.data_ptr(), kc_scale.data_ptr(),
+            v_cache.data_ptr(), v_scale.data_ptr(), outs[0], outs[1], outs[2], kt, vt)
+    return seq_len
+
+
+def sfa_attn_decode_q4_workspace(B: int, Hq: int, Lmax: int, d: int) -> int:
+    """Bytes of device workspace sfa_attn_decode_q4 needs."""
+    return int(lib().sfa_attn_decode_q4_workspace(B, Hq, Lmax, d))
+
+
+def sfa_attn_decode_q4(kc_idx, kc_val, kc_scale, v_cache, v_scale, block_table=None, seq_len=None,
+                       q=None, q_idx=None, q_val=None, scale: float | None = None,
+                       o_dtype=torch.float32, o=None, lse=None, want_lse: bool = True, ws=None,
+                       window: int = 0, n_global: int = 0):
+    """Decode over a 4-bit cache (contiguous, or paged with block_table), with query
+    codes q_idx / q_val [B, Hq, k] or a dense float32 query q [B, Hq, d] coded in the
+    kernel.  Returns (o [B, Hq, d], lse [B, Hq] or None)."""
+    pages, Hkv, P, k, d = _q4_cache(kc_idx, kc_val, kc_scale, v_cache, v_scale)
+    qp = qip = qvp = qit = qvt = 0
+    if q is not None:
+        if q_idx is not None or q_val is not None:
+            raise ValueError("give either q or (q_idx, q_val)")
+        _check(q, "q", _F32)
+        if q.dim() != 3 or q.shape[2] != d:
+            raise ValueError("q must be [B, Hq, d]")
+        B, Hq = q.shape[:2]
+        qp = q.data_ptr()
+    else:
+        qit = _check(q_idx, "q_idx", _IDX); qvt = _check(q_val, "q_val", _CVAL)
+        if q_idx.dim() != 3 or q_idx.shape[2] != k or tuple(q_val.shape) != tuple(q_idx.shape):
+            raise ValueError("q codes must be [B, Hq, k]")
+        B, Hq = q_idx.shape[:2]
+        qip, qvp = q_idx.data_ptr(), q_val.data_ptr()
+    tp, maxp, cap = 0, 0, P
+    if block_table is not None:
+        _check(block_table, "block_table", _I32)
+        if block_table.dim() != 2 or block_table.shape[0] != B:
+            raise ValueError("block_table must be [B, max_pages]")
+        tp, maxp = block_table.data_ptr(), block_table.shape[1]
+        cap = maxp * P
+    elif pages != B:
+        raise ValueError("a contiguous cache holds B sequences")
+    sp = _i32_vec(seq_len, "seq_len", B) if seq_len is not None else 0
+    if scale is None:
+        scale = 1.0 / math.sqrt(d)
+    if o is None:
+        o = torch.empty((B, Hq, d), dtype=o_dtype, device=v_cache.device)
+    ot = _check(o, "o", _VAL)
+    if tuple(o.shape) != (B, Hq, d):
+        raise ValueError("o has the wrong shape")
+    if lse is None and want_lse:
+        lse = torch.empty((B, Hq), dtype=torch.float32, device=v_cache.device)
+    if lse is not None:
+        _check(lse, "lse", _F32)
+        if lse.numel() != B * Hq:
+            raise ValueError("lse must hold B * Hq entries")
+    if ws is None:
+        ws = torch.empty(sfa_attn_decode_q4_workspace(B, Hq, cap, d), dtype=torch.uint8,
+                         device=v_cache.device)
+    if not ws.is_contiguous():
+        raise ValueError("ws must be contiguous")
+    _together(kc_idx, q=q, q_idx=q_idx, q_val=q_val, block_table=block_table, seq_len=seq_len, o=o,
+              lse=lse, ws=ws)
+    _launch(kc_idx, "sfa_attn_decode_q4", qp, qip, qvp, kc_idx.data_ptr(), kc_val.data_ptr(),
+            kc_scale.data_ptr(), v_cache.data_ptr(), v_scale.data_ptr(), tp, maxp, P, pages, sp, B,
+            Hq, Hkv, d, k, float(scale), int(window), int(n_global), qit, qvt, ot, o.data_ptr(),
+            lse.data_ptr() if lse is not None else 0, ws.data_ptr(), ws.numel() * ws.element_size())
+    return o, lse

@@ -243,9 +243,14 @@ hipError_t launch_kv_append(const AppendArgs& a, hipStream_t stream) {
     const hipError_t e = launch_append<false>(a, dim3(gx, gy), dim3(256), stream);
     if (e != hipSuccess) return e;
   }
-  const int64_t cap = a.table ? (int64_t)a.max_pages * a.page_size : a.page_size;
-  hipLaunchKernelGGL(sfa_kv_advance_kernel, dim3((a.B + 255) / 256), dim3(256), 0, stream,
-                     a.seq_len, a.n_new, a.B, a.T, cap);
+  return launch_kv_advance(a.seq_len, a.n_new, a.B, a.T,
+                           a.table ? (int64_t)a.max_pages * a.page_size : a.page_size, stream);
+}
+
+hipError_t launch_kv_advance(int32_t* seq_len, const int32_t* n_new, int B, int T, int64_t cap,
+                             hipStream_t stream) {
+  hipLaunchKernelGGL(sfa_kv_advance_kernel, dim3((B + 255) / 256), dim3(256), 0, stream, seq_len,
+                     n_new, B, T, cap);
   return hipGetLastError();
 }
 

@@ -75,6 +75,7 @@ struct DecodeArgs {
   // 8-bit cache (launch_attn_decode_q8): float32 scale per key row / value row
   const float* kc_scale;
   const float* v_scale;
+  const uint16_t* v_scale16;  // 4-bit cache (launch_attn_decode_q4): bfloat16 scale per 32 values
 };
 // Most keys of a decode workgroup (one context chunk), and of the float32
 // decode's; the workspace holds one partial (m, l, o) per chunk, query head
@@ -103,6 +104,8 @@ inline int decode_slots(int span, int aim) {
   return fine < most ? fine : most;
 }
 hipError_t launch_attn_decode(const DecodeArgs& a, hipStream_t stream);
+// The most partial slots of a step over Lmax keys with that aim, windowed or not.
+int decode_most_slots(int Lmax, int aim);
 // Workspace of any step of these sizes, and of one in chunks of kDecodeChunk
 // keys (never more than the former).
 size_t decode_workspace_bytes(int B, int Hq, int Lmax, int d);
@@ -162,5 +165,66 @@ struct CsrArgs {
   void* val_out;
 };
 hipError_t launch_csr_to_codes(const CsrArgs& a, hipStream_t stream);
+
+// Rotary positions (the device's part of an sfa_rope_plan).
+struct RopePlan {
+  int d, rot;
+  int neighbours;  // pairs (2i, 2i + 1) rather than (i, i + rot/2)
+  int inverse;     // turn back
+  double freq[128];
+  uint8_t axis[128];
+};
+struct RopeArgs {
+  const void* x;
+  int64_t xs[3], ys[3];  // element strides of batch, head, token
+  const int32_t* pos;
+  int64_t pos_axis, pos_batch;
+  int B, H, n, d, k;
+  int xbf16, ybf16;
+  void* y;  // rotated rows, or the backward's dx
+  void *idx, *val;
+  const float* dval;
+  int ifmt, vfmt;
+  int units, heads, tokens;  // set by the launchers
+};
+hipError_t launch_rope(const RopePlan& pl, RopeArgs a, hipStream_t stream);
+hipError_t launch_rope_encode(const RopePlan& pl, RopeArgs a, hipStream_t stream);
+hipError_t launch_rope_encode_bwd(const RopePlan& pl, RopeArgs a, hipStream_t stream);
+
+// Block tables, free list and slot map from old and new lengths.
+struct PageArgs {
+  const int32_t *old_len, *new_len, *free_in;
+  int32_t *table, *free_pages, *free_out, *got, *starts, *slots, *pos;
+  int B, max_pages, log2P, num_pages, n_rows;
+  int32_t* ws;
+};
+size_t page_tables_workspace_bytes(int B);
+hipError_t launch_page_tables(const PageArgs& a, hipStream_t stream);
+
+// Append to the 4-bit cache.
+struct AppendQ4Args {
+  const void *k_new, *v_new;
+  int64_t st[6];  // element strides: k batch, head, token, v batch, head, token
+  const int32_t *slots, *n_new, *table;
+  int32_t* seq_len;
+  int B, Hkv, T, d, k;
+  int max_pages, page_size, num_pages;
+  int kbf16, vbf16;
+  uint8_t *kc_idx, *kc_val, *v_cache;
+  float* kc_scale;
+  uint16_t* v_scale;
+  int16_t* k_idx;
+  float* k_val;
+  uint16_t* v_out;
+};
+hipError_t launch_kv_append_q4(const AppendQ4Args& a, hipStream_t stream);
+// seq_len[b] += the appended count, clamped to the capacity (sfa_cache.hip)
+hipError_t launch_kv_advance(int32_t* seq_len, const int32_t* n_new, int B, int T, int64_t cap,
+                             hipStream_t stream);
+
+// Decode over the 4-bit cache (DecodeArgs: kc_val, v, kc_scale and v_scale16 its
+// arrays, aim from decode_chunks_aim).
+size_t decode_q4_workspace_bytes(int B, int Hq, int Lmax, int d);
+hipError_t launch_attn_decode_q4(const DecodeArgs& a, hipStream_t stream);
 
 }  // namespace sfa
