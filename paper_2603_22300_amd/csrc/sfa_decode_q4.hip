@@ -56,7 +56,7 @@ __device__ __forceinline__ f16x8 nibbles_f16(uint32_t x) {
 // D: head dimension, or 256 for any d <= 256 (p.d then counts).  GP: query heads
 // per KV head rounded up to 4 or 8.  KC8: k / 8, or 0 to take it from p.k.
 template <int D, int GP, int KC8, bool PAGED>
-__global__ __launch_bounds__(kDecThreads) void sfa_decode_q4_kernel(DecParams p, int dd, const uint16_t* vscale) {
+__global__ __launch_bounds__(kDecThreads, GP == 4 && D <= 128 ? 3 : GP == 8 && D <= 128 ? 2 : 1) void sfa_decode_q4_kernel(DecParams p, int dd, const uint16_t* vscale) {
   constexpr int NG = D / 32;              // value scale groups, two 16-coordinate tiles each
   constexpr int PITCH = D / 2 + 8;        // bytes of a value row in LDS: rows on different banks
   const int d = D == 256 ? dd : D, ng = d / 32;
@@ -158,26 +158,55 @@ __global__ __launch_bounds__(kDecThreads) void sfa_decode_q4_kernel(DecParams p,
 
   unsigned char* vw = vt[wave];
   const uint8_t* vc = (const uint8_t*)p.v;
-  for (int sb = w0; sb < w1; sb += 64) {
-    const int64_t row = row_of(min(sb + lane, w1 - 1));
-    // the value rows, 16 bytes a lane: piece x of the 64 rows' 64 d / 32 pieces
-    for (int x = lane; x < 64 * ng; x += 64) {
-      const int jj = x / ng, piece = x - jj * ng;
+  // A block of 64 keys in registers, loaded one block ahead: value rows (16 bytes a
+  // lane and load, piece x of the rows' 64 d / 32 pieces), and lane = key: codes
+  // (KC8 > 0), scales.
+  constexpr int NKC = KC8 > 0 ? KC8 : 1;
+  uint4 vraw[NG];
+  uint2 ki[NKC];
+  uint32_t kq[NKC], vs_next[NG];
+  float ks_next = 0.f;
+  int64_t row = 0;
+  auto load_values = [&](int sb) {
+    row = row_of(min(sb + lane, w1 - 1));
+#pragma unroll
+    for (int i = 0; i < NG; ++i) {
+      if (i >= ng) break;
+      const int x = lane + 64 * i, jj = x / ng, piece = x - jj * ng;
       const int64_t vr = PAGED ? (int64_t)__shfl(row, jj, 64) : kv_row0 + min(sb + jj, w1 - 1);
-      const uint4 w = *(const uint4*)(vc + vr * (d / 2) + piece * 16);
-      uint2* dst = (uint2*)(vw + jj * PITCH + piece * 16);
-      dst[0] = make_uint2(w.x, w.y);
-      dst[1] = make_uint2(w.z, w.w);
+      vraw[i] = *(const uint4*)(vc + vr * (d / 2) + piece * 16);
     }
+  };
+  auto load_codes = [&]() {  // of the rows that load_values went to
+    if constexpr (KC8 > 0) {
+#pragma unroll
+      for (int c = 0; c < KC8; ++c) {
+        ki[c] = ((const uint2*)((const uint8_t*)p.kc_idx + row * k))[c];
+        kq[c] = ((const uint32_t*)((const uint8_t*)p.kc_val + row * (k / 2)))[c];
+      }
+    }
+    ks_next = p.kc_scale[row];
+#pragma unroll
+    for (int g = 0; g < NG; ++g) vs_next[g] = g < ng ? vscale[row * ng + g] : 0;
+  };
+  if (w0 < w1) { load_values(w0); load_codes(); }
+  for (int sb = w0; sb < w1; sb += 64) {
+#pragma unroll
+    for (int i = 0; i < NG; ++i) {
+      if (i >= ng) break;
+      const int x = lane + 64 * i, jj = x / ng, piece = x - jj * ng;
+      uint2* dst = (uint2*)(vw + jj * PITCH + piece * 16);
+      dst[0] = make_uint2(vraw[i].x, vraw[i].y);
+      dst[1] = make_uint2(vraw[i].z, vraw[i].w);
+    }
+    const int64_t row_here = row;
+    const bool more = sb + 64 < w1;
+    if (more) load_values(sb + 64);
     // scores
     float s[GP];
 #pragma unroll
     for (int h = 0; h < GP; ++h) s[h] = 0.f;
-    const uint2* ki = (const uint2*)((const uint8_t*)p.kc_idx + row * k);
-    const uint32_t* kq = (const uint32_t*)((const uint8_t*)p.kc_val + row * (k / 2));
-    for (int c8 = 0; c8 < k / 8; ++c8) {
-      const uint2 iw = ki[c8];
-      const uint32_t qw = kq[c8];
+    auto score8 = [&](uint2 iw, uint32_t qw) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const int u = min((int)(((e < 4 ? iw.x : iw.y) >> (8 * (e & 3))) & 255u), d - 1);
@@ -185,10 +214,22 @@ __global__ __launch_bounds__(kDecThreads) void sfa_decode_q4_kernel(DecParams p,
 #pragma unroll
         for (int h = 0; h < GP; ++h) s[h] = fmaf(kv, qd[u][h], s[h]);
       }
+    };
+    if constexpr (KC8 > 0) {
+#pragma unroll
+      for (int c = 0; c < KC8; ++c) score8(ki[c], kq[c]);
+    } else {
+      for (int c = 0; c < k / 8; ++c)
+        score8(((const uint2*)((const uint8_t*)p.kc_idx + row_here * k))[c],
+               ((const uint32_t*)((const uint8_t*)p.kc_val + row_here * (k / 2)))[c]);
     }
-    const float kfac = p.scale_log2 * p.kc_scale[row];
-    const bool ok = sb + lane < w1 && key_ok(sb + lane);
+    const float ks = ks_next;
     uint32_t vsb[NG];
+#pragma unroll
+    for (int g = 0; g < NG; ++g) vsb[g] = vs_next[g];
+    if (more) load_codes();
+    const float kfac = p.scale_log2 * ks;
+    const bool ok = sb + lane < w1 && key_ok(sb + lane);
     float t[GP];
     bool up = false;  // this lane's key passes a running maximum by 2^8, or a group's exponent
 #pragma unroll
@@ -198,7 +239,7 @@ __global__ __launch_bounds__(kDecThreads) void sfa_decode_q4_kernel(DecParams p,
     }
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
-      vsb[g] = g < ng && ok ? vscale[row * ng + g] & 0x7fffu : 0u;
+      vsb[g] = ok ? vsb[g] & 0x7fffu : 0u;
       up |= (int)(vsb[g] >> 7) > vexp[g];
     }
     if (wave_ballot(up)) {  // uniform; the first block always
@@ -286,11 +327,15 @@ __global__ __launch_bounds__(kDecThreads) void sfa_decode_q4_kernel(DecParams p,
 #pragma unroll
   for (int t = 0; t < 2 * NG; ++t)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float x = acc[t][i] + __shfl_xor(acc[t][i], 4 * GP, 64);
-      const int h = GP == 4 ? i : 4 * ((lane >> 4) & 1) + i;
-      if (lane < 4 * GP) red_o[(wave * GP + h) * D + 16 * t + (lane & 15)] = x * __uint_as_float((uint32_t)(vexp[t / 2] - 5) << 23);
-    }
+    for (int i = 0; i < 4; ++i)
+      acc[t][i] = (acc[t][i] + __shfl_xor(acc[t][i], 4 * GP, 64)) * __uint_as_float((uint32_t)(vexp[t / 2] - 5) << 23);
+  if (lane < 4 * GP) {
+    const int h0 = GP == 4 ? 0 : 4 * (lane >> 4);
+#pragma unroll
+    for (int t = 0; t < 2 * NG; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) red_o[(wave * GP + h0 + i) * D + 16 * t + (lane & 15)] = acc[t][i];
+  }
   if (lane == 0) {
 #pragma unroll
     for (int h = 0; h < GP; ++h) { red_m[wave][h] = m_run[h]; red_l[wave][h] = l_lane[h]; }
