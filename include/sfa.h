@@ -706,8 +706,8 @@ sfa_status sfa_kv_append_q4(const void* k_new, const void* v_new, const int64_t*
  * sfa_attn_decode_q8; a sequence with 0 keys gets O = 0 and LSE = -inf.
  * ws: sfa_attn_decode_q4_workspace(B, Hq, capacity, d) bytes, scratch.
  * Limits: d a multiple of 32, k a multiple of 8, k <= d <= 256, Hq / Hkv <= 8 (any
- *         group; SFA_ENOTSUP otherwise); cache arrays 16-byte aligned (the scales 4
- *         and 2); paged: page_size a power of two >= 16; capacity <= 2^30;
+ *         group; SFA_ENOTSUP otherwise); the five cache arrays 16-byte aligned;
+ *         paged: page_size a power of two >= 16; capacity <= 2^30;
  *         B * Hkv <= 65535.
  * Errors: SFA_EINVAL, SFA_ENOTSUP, SFA_ENOSPC, SFA_EHIP.
  */

@@ -630,8 +630,8 @@ sfa_status sfa_attn_decode_q4(const float* q, const void* q_idx, const void* q_v
   if (cap > (1LL << 30)) return SFA_ENOTSUP;
   if ((long long)B * Hkv > 65535) return SFA_ENOTSUP;
   if (d > 256 || d % 32 != 0 || k % 8 != 0 || Hq / Hkv > sfa::decode_max_group()) return SFA_ENOTSUP;
-  if (((uintptr_t)v_cache | (uintptr_t)kc_idx | (uintptr_t)kc_val) % 16 != 0 || (uintptr_t)kc_scale % 4 != 0 ||
-      (uintptr_t)v_scale % 2 != 0 || (uintptr_t)ws % 4 != 0)
+  if (((uintptr_t)v_cache | (uintptr_t)kc_idx | (uintptr_t)kc_val | (uintptr_t)kc_scale | (uintptr_t)v_scale) % 16 != 0 ||
+      (uintptr_t)ws % 4 != 0)
     return SFA_EINVAL;
   const int Lmax = (int)cap;
   if (ws_bytes < sfa::decode_q4_workspace_bytes(B, Hq, Lmax, d)) return SFA_ENOSPC;

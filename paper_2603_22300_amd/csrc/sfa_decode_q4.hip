@@ -13,15 +13,22 @@
 //            f16(p vs) and p1 = f16(p vs - p0): the pieces of the group's query
 //            heads fill the sixteen rows of one operand, so the second piece (and
 //            with it float32 accuracy, 2^-22) costs no matrix instruction.  The
-//            other operand is the cached integers, exact in float16.
+//            other operand is the cached numbers: a nibble with its sign flipped is
+//            q + 8, and set into the low mantissa bits of a float16 it is (q + 8)
+//            2^-24, or 16 times that at bit 4 (odd keys; their weights carry 1/16):
+//            subnormal numbers, which the matrix cores keep.  One instruction per
+//            two numbers; a second matrix instruction with a constant operand takes
+//            the 8 off again, block by block, so that the sums stay small.
 // Both operands have 16 or 8 keys of one row in a lane, and both are held key by
 // key: the transposing LDS reads turn them, ds_read_b64_tr_b4 the cached nibbles
-// as they are and ds_read_b64_tr_b16 the weights.
+// as they are and ds_read_b64_tr_b16 the weights.  Value rows go to LDS directly
+// (global_load_lds), one block of keys ahead, the 16-byte pieces of a row exchanged
+// so that the transposing reads find each key on banks of its own.
 //
 // float16 range: each group's weights are scaled by a power of two that follows
 // the largest value scale seen in the group, as the running maximum does for p
-// (`vexp` below): value scales of any magnitude keep their accuracy.  Both follow
-// lazily, p up to 2^8 and only upwards for the scales, so that most blocks of keys
+// (`vexp` below): value scales from 2^-116 up keep their accuracy.  Both follow
+// lazily, p up to 2^4 and only upwards for the scales, so that most blocks of keys
 // touch neither the maxima nor the accumulators.
 #include "sfa_decode_kernel.h"
 
@@ -30,7 +37,6 @@ namespace {
 
 typedef int v2i __attribute__((ext_vector_type(2)));
 typedef short v4s __attribute__((ext_vector_type(4)));
-typedef _Float16 h2 __attribute__((ext_vector_type(2)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 
 __device__ __forceinline__ v2i read_tr4(const void* p) {
@@ -40,29 +46,29 @@ __device__ __forceinline__ v4s read_tr16(const void* p) {
   return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)p);
 }
 
-// Eight nibbles (two's complement) as float16, in the order n0 n4 n1 n5 n2 n6 n3
-// n7.  A nibble with its sign bit flipped is q + 8; at the low end of a float16
-// mantissa under exponent 2^10 it adds itself to 1024, at bit 4 under 2^6 to 64.
+// Eight nibbles (two's complement), each as (q + 8) 2^-24 in float16, those of odd
+// keys 16 times that, in the order n0 n4 n1 n5 n2 n6 n3 n7.
 __device__ __forceinline__ f16x8 nibbles_f16(uint32_t x) {
   const uint32_t y = x >> 8;
-  const h2 lo = {(_Float16)1032.f, (_Float16)1032.f}, hi = {(_Float16)72.f, (_Float16)72.f};
-  const h2 a = __builtin_bit_cast(h2, (x & 0x000f000fu) ^ 0x64086408u) - lo;
-  const h2 b = __builtin_bit_cast(h2, (x & 0x00f000f0u) ^ 0x54805480u) - hi;
-  const h2 c = __builtin_bit_cast(h2, (y & 0x000f000fu) ^ 0x64086408u) - lo;
-  const h2 d = __builtin_bit_cast(h2, (y & 0x00f000f0u) ^ 0x54805480u) - hi;
-  return f16x8{a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y};
+  const u32x4 r = {(x & 0x000f000fu) ^ 0x00080008u, (x & 0x00f000f0u) ^ 0x00800080u,
+                   (y & 0x000f000fu) ^ 0x00080008u, (y & 0x00f000f0u) ^ 0x00800080u};
+  return __builtin_bit_cast(f16x8, r);
 }
 
-// D: head dimension, or 256 for any d <= 256 (p.d then counts).  GP: query heads
+__device__ __forceinline__ float pow2_field(int field) { return __uint_as_float((uint32_t)field << 23); }
+
+// D: head dimension, or 256 for any d <= 256 (dd then counts).  GP: query heads
 // per KV head rounded up to 4 or 8.  KC8: k / 8, or 0 to take it from p.k.
-template <int D, int GP, int KC8, bool PAGED>
-__global__ __launch_bounds__(kDecThreads, GP == 4 && D <= 128 ? 3 : GP == 8 && D <= 128 ? 2 : 1) void sfa_decode_q4_kernel(DecParams p, int dd, const uint16_t* vscale) {
-  constexpr int NG = D / 32;              // value scale groups, two 16-coordinate tiles each
-  constexpr int PITCH = D / 2 + 8;        // bytes of a value row in LDS: rows on different banks
+// PG: 0 contiguous, 1 pages of 64 positions or more (a block of keys has one), 2
+// pages of 16 or 32.
+template <int D, int GP, int KC8, int PG>
+__global__ __launch_bounds__(kDecThreads, GP == 4 && D <= 128 ? 3 : GP == 8 && D <= 128 ? 2 : 1)
+void sfa_decode_q4_kernel(DecParams p, int dd, const uint16_t* vscale) {
+  constexpr int NG = D / 32;  // value scale groups, two 16-coordinate tiles each
   const int d = D == 256 ? dd : D, ng = d / 32;
   const int k = KC8 > 0 ? 8 * KC8 : p.k;
-  __shared__ float qd[D][GP];
-  __shared__ __attribute__((aligned(16))) unsigned char vt[kDecWaves][64 * PITCH];
+  __shared__ float qd[256][GP];  // (an index past d reads zeros)
+  __shared__ __attribute__((aligned(16))) unsigned char vt[kDecWaves][64 * D / 2];
   __shared__ __attribute__((aligned(16))) _Float16 pb[kDecWaves][NG][64][2 * GP];
   __shared__ float red_m[kDecWaves][GP], red_l[kDecWaves][GP];
 
@@ -85,10 +91,12 @@ __global__ __launch_bounds__(kDecThreads, GP == 4 && D <= 128 ? 3 : GP == 8 && D
   const int c1 = min(L, c0 + plan.c);
 
   // dense query rows
+  for (int x = tid; x < 256 * GP; x += kDecThreads) (&qd[0][0])[x] = 0.f;
+  __syncthreads();
   if (p.q_dense) {
     constexpr int E = (D + 63) / 64;
-    for (int h = wave; h < GP; h += kDecWaves) {
-      const float* qr = p.q_dense + ((int64_t)b * p.Hq + hkv * p.G + min(h, p.G - 1)) * d;
+    for (int h = wave; h < p.G; h += kDecWaves) {
+      const float* qr = p.q_dense + ((int64_t)b * p.Hq + hkv * p.G + h) * d;
       uint32_t bits[E], key[E];
       bool sel[E];
 #pragma unroll
@@ -100,11 +108,9 @@ __global__ __launch_bounds__(kDecThreads, GP == 4 && D <= 128 ? 3 : GP == 8 && D
       topk_select<E>(key, k, sel);
 #pragma unroll
       for (int e = 0; e < E; ++e)
-        if (lane + 64 * e < D) qd[lane + 64 * e][h] = sel[e] && h < p.G ? __uint_as_float(bits[e]) : 0.f;
+        if (sel[e] && lane + 64 * e < d) qd[lane + 64 * e][h] = __uint_as_float(bits[e]);
     }
   } else {
-    for (int x = tid; x < D * GP; x += kDecThreads) (&qd[0][0])[x] = 0.f;
-    __syncthreads();
     for (int x = tid; x < p.G * k; x += kDecThreads) {
       const int h = x / k, t = x - h * k;
       const int64_t qi = ((int64_t)b * p.Hq + hkv * p.G + h) * k + t;
@@ -114,33 +120,33 @@ __global__ __launch_bounds__(kDecThreads, GP == 4 && D <= 128 ? 3 : GP == 8 && D
   }
   __syncthreads();
 
-  float m_run[GP], l_lane[GP];
+  float m_run[GP], m_use[GP], l_lane[GP];  // m_use: m_run, or 0 before the first key
 #pragma unroll
-  for (int h = 0; h < GP; ++h) { m_run[h] = -INFINITY; l_lane[h] = 0.f; }
+  for (int h = 0; h < GP; ++h) { m_run[h] = -INFINITY; m_use[h] = 0.f; l_lane[h] = 0.f; }
   floatx4 acc[2 * NG];
 #pragma unroll
   for (int t = 0; t < 2 * NG; ++t) acc[t] = floatx4{0.f, 0.f, 0.f, 0.f};
-  // Per group, the exponent field of the largest value scale seen, at least 6; the
-  // weights carry 2^(132 - vexp) (a scale of that exponent field becomes 2^5 to 2^6,
-  // a weight at most 2^14).
+  // Per group, the exponent field of the largest value scale seen, at least 11; the
+  // weights of even keys carry 2^(137 - vexp): a scale of that exponent field becomes
+  // 2^10 to 2^11 and a weight at most 2^15, and the smallest weight that the second
+  // piece still holds is 2^-34 of p = 1 (2^-30 for odd keys).
   int vexp[NG];
 #pragma unroll
-  for (int g = 0; g < NG; ++g) vexp[g] = 6;
+  for (int g = 0; g < NG; ++g) vexp[g] = 11;
 
   const int64_t kv_row0 = ((int64_t)b * p.Hkv + hkv) * p.Lmax;
   const int per_wave = plan.c / kDecWaves;
-  int w0 = c0 + wave * per_wave;
+  int w0 = c0 + wave * per_wave;  // a multiple of 64
   int w1 = min(c1, w0 + per_wave);
   if (winq && w0 >= wg) {
     if (w1 <= wlo) w1 = w0;
     else w0 = max(w0, wlo & ~63);
   }
-  auto key_ok = [&](int j) { return j >= wlo || j < wg; };
   // paged: lane l holds the page of the wave's l-th page-sized run (at most 1024
   // positions and pages of 16 or more: at most 64 runs)
   int tblv = 0;
-  const int pg0 = PAGED ? (w0 >> p.log2P) : 0;
-  if constexpr (PAGED) {
+  const int pg0 = PG ? (w0 >> p.log2P) : 0;
+  if constexpr (PG > 0) {
     if (w0 < w1) {
       const int npg = ((w1 - 1) >> p.log2P) - pg0 + 1;
       if (lane < npg) {
@@ -149,68 +155,109 @@ __global__ __launch_bounds__(kDecThreads, GP == 4 && D <= 128 ? 3 : GP == 8 && D
       }
     }
   }
-  const int pmask = (1 << (PAGED ? p.log2P : 0)) - 1;
-  auto row_of = [&](int j) -> int64_t {  // w0 <= j < w1, any j per lane
-    if constexpr (PAGED)
-      return (((int64_t)__shfl(tblv, (j >> p.log2P) - pg0, 64) * p.Hkv + hkv) << p.log2P) + (j & pmask);
-    else return kv_row0 + j;
+  const int pmask = (1 << (PG ? p.log2P : 0)) - 1;
+  // the cache row of position j on page pg
+  auto paged_row = [&](int pg, int j) -> int64_t { return (((int64_t)pg * p.Hkv + hkv) << p.log2P) + (j & pmask); };
+  // the row of a block's first key, where the others follow it (PG < 2)
+  auto block_row = [&](int sb) -> int64_t {
+    if constexpr (PG == 1) return paged_row(__builtin_amdgcn_readlane(tblv, (sb >> p.log2P) - pg0), sb);
+    else return kv_row0 + sb;
   };
 
+  // Value rows, to LDS directly: 16-byte piece x of the block's 64 ng, x = lane + 64 i,
+  // belongs to key x / ng and holds its piece (x % ng) ^ ((key / (16 / ng)) % ng) (ng a
+  // power of two; the others keep their order).
   unsigned char* vw = vt[wave];
+  const int sw_mask = (ng & (ng - 1)) == 0 ? ng - 1 : 0;
+  const int sw_shift = ng >= 8 ? 1 : ng >= 4 ? 2 : ng >= 2 ? 3 : 4;
   const uint8_t* vc = (const uint8_t*)p.v;
-  // A block of 64 keys in registers, loaded one block ahead: value rows (16 bytes a
-  // lane and load, piece x of the rows' 64 d / 32 pieces), and lane = key: codes
-  // (KC8 > 0), scales.
-  constexpr int NKC = KC8 > 0 ? KC8 : 1;
-  uint4 vraw[NG];
-  uint2 ki[NKC];
-  uint32_t kq[NKC], vs_next[NG];
-  float ks_next = 0.f;
-  int64_t row = 0;
-  auto load_values = [&](int sb) {
-    row = row_of(min(sb + lane, w1 - 1));
+  auto load_values = [&](int sb, int page) {  // page: of this lane's key (PG 2)
+    const int last = w1 - 1 - sb;
+    const uint8_t* base = PG < 2 ? vc + block_row(sb) * (d / 2) : nullptr;
 #pragma unroll
     for (int i = 0; i < NG; ++i) {
       if (i >= ng) break;
-      const int x = lane + 64 * i, jj = x / ng, piece = x - jj * ng;
-      const int64_t vr = PAGED ? (int64_t)__shfl(row, jj, 64) : kv_row0 + min(sb + jj, w1 - 1);
-      vraw[i] = *(const uint4*)(vc + vr * (d / 2) + piece * 16);
+      const int x = lane + 64 * i, key = x / ng;
+      const int piece = (x - key * ng) ^ ((key >> sw_shift) & sw_mask);
+      const uint8_t* src;
+      if constexpr (PG < 2) {
+        src = base + (uint32_t)((last >= 63 ? key : min(key, last)) * (d / 2) + piece * 16);
+      } else {
+        const int kc = min(key, last);
+        src = vc + paged_row(__shfl(page, kc, 64), sb + kc) * (d / 2) + piece * 16;
+      }
+      __builtin_amdgcn_global_load_lds(src, (__attribute__((address_space(3))) void*)(vw + i * 1024), 16, 0, 0);
     }
   };
-  auto load_codes = [&]() {  // of the rows that load_values went to
+  // A key's codes and scales (lane = key), loaded a block ahead.
+  constexpr int NKC = KC8 > 0 ? KC8 : 1;
+  uint2 ki[NKC], ki2[NKC];
+  uint32_t kq[NKC], kq2[NKC], vs[NG], vs2[NG];
+  float ks = 0.f, ks2 = 0.f;
+  auto lane_row = [&](int sb, int page) -> int64_t {
+    const int kc = min(lane, w1 - 1 - sb);
+    return PG < 2 ? block_row(sb) + kc : paged_row(page, sb + kc);
+  };
+  auto load_codes = [&](int sb, int page, uint2 (&ki)[NKC], uint32_t (&kq)[NKC], float& ks, uint32_t (&vs)[NG]) {
+    const int64_t row = PG < 2 ? block_row(sb) : lane_row(sb, page);
+    const uint32_t o = PG < 2 ? (uint32_t)min(lane, w1 - 1 - sb) : 0u;
     if constexpr (KC8 > 0) {
+      const uint8_t* pi = (const uint8_t*)p.kc_idx + row * k + o * k;
+      const uint8_t* pq = (const uint8_t*)p.kc_val + row * (k / 2) + o * (k / 2);
 #pragma unroll
       for (int c = 0; c < KC8; ++c) {
-        ki[c] = ((const uint2*)((const uint8_t*)p.kc_idx + row * k))[c];
-        kq[c] = ((const uint32_t*)((const uint8_t*)p.kc_val + row * (k / 2)))[c];
+        ki[c] = ((const uint2*)pi)[c];
+        kq[c] = ((const uint32_t*)pq)[c];
       }
     }
-    ks_next = p.kc_scale[row];
+    ks = (p.kc_scale + row)[o];
+    const uint16_t* pv = vscale + row * ng + o * ng;
+    if constexpr (D == 128) {
+      const uint2 w = *(const uint2*)pv;
+      vs[0] = w.x & 0xffffu; vs[1] = w.x >> 16; vs[2] = w.y & 0xffffu; vs[3] = w.y >> 16;
+    } else if constexpr (D == 64) {
+      const uint32_t w = *(const uint32_t*)pv;
+      vs[0] = w & 0xffffu; vs[1] = w >> 16;
+    } else {
 #pragma unroll
-    for (int g = 0; g < NG; ++g) vs_next[g] = g < ng ? vscale[row * ng + g] : 0;
-  };
-  if (w0 < w1) { load_values(w0); load_codes(); }
-  for (int sb = w0; sb < w1; sb += 64) {
-#pragma unroll
-    for (int i = 0; i < NG; ++i) {
-      if (i >= ng) break;
-      const int x = lane + 64 * i, jj = x / ng, piece = x - jj * ng;
-      uint2* dst = (uint2*)(vw + jj * PITCH + piece * 16);
-      dst[0] = make_uint2(vraw[i].x, vraw[i].y);
-      dst[1] = make_uint2(vraw[i].z, vraw[i].w);
+      for (int g = 0; g < NG; ++g) vs[g] = g < ng ? pv[g] : 0;
     }
-    const int64_t row_here = row;
-    const bool more = sb + 64 < w1;
-    if (more) load_values(sb + 64);
-    // scores
+  };
+  auto page_of = [&](int sb) -> int {
+    if constexpr (PG == 2) return __shfl(tblv, (min(sb + lane, w1 - 1) >> p.log2P) - pg0, 64);
+    else return 0;
+  };
+  // operand addresses in LDS (see the P.V loop)
+  const int r16 = lane & 15, key0 = lane & 48;
+  const _Float16* a_src = &pb[wave][0][key0 + (r16 >> 3) + 4 * ((r16 >> 2) & 1)][4 * ((r16 & 3) & (GP / 2 - 1))];
+  const unsigned char* b_src[NG];
+#pragma unroll
+  for (int g = 0; g < NG; ++g)
+    b_src[g] = vw + (key0 + r16) * (d / 2) + (g ^ ((r16 >> sw_shift) & sw_mask)) * 16;
+  const u32x4 minus8 = {0x80088008u, 0x80808080u, 0x80088008u, 0x80808080u};
+  const int odd4 = 4 * (lane & 1);
+
+  int page = 0;
+  if (w0 < w1) {
+    page = page_of(w0);
+    load_codes(w0, page, ki, kq, ks, vs);
+    load_values(w0, page);
+  }
+  for (int sb = w0; sb < w1; sb += 64) {
+    const int last = w1 - 1 - sb;
+    const bool more = last >= 64;
+    const int page_next = more ? page_of(sb + 64) : 0;
+    if (more) load_codes(sb + 64, page_next, ki2, kq2, ks2, vs2);
+    // scores: the code values count in sixteenths (v_cvt_off_f32_i4)
     float s[GP];
 #pragma unroll
     for (int h = 0; h < GP; ++h) s[h] = 0.f;
     auto score8 = [&](uint2 iw, uint32_t qw) {
+      const uint32_t qh = qw >> 4;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const int u = min((int)(((e < 4 ? iw.x : iw.y) >> (8 * (e & 3))) & 255u), d - 1);
-        const float kv = (float)((int)(qw << (28 - 4 * e)) >> 28);
+        const int u = (int)(((e < 4 ? iw.x : iw.y) >> (8 * (e & 3))) & 255u);
+        const float kv = __builtin_amdgcn_cvt_off_f32_i4((int)((((e & 1) ? qh : qw) >> (8 * (e >> 1))) & 255u));
 #pragma unroll
         for (int h = 0; h < GP; ++h) s[h] = fmaf(kv, qd[u][h], s[h]);
       }
@@ -219,47 +266,49 @@ __global__ __launch_bounds__(kDecThreads, GP == 4 && D <= 128 ? 3 : GP == 8 && D
 #pragma unroll
       for (int c = 0; c < KC8; ++c) score8(ki[c], kq[c]);
     } else {
+      const int64_t row = lane_row(sb, page);
       for (int c = 0; c < k / 8; ++c)
-        score8(((const uint2*)((const uint8_t*)p.kc_idx + row_here * k))[c],
-               ((const uint32_t*)((const uint8_t*)p.kc_val + row_here * (k / 2)))[c]);
+        score8(((const uint2*)((const uint8_t*)p.kc_idx + row * k))[c],
+               ((const uint32_t*)((const uint8_t*)p.kc_val + row * (k / 2)))[c]);
     }
-    const float ks = ks_next;
-    uint32_t vsb[NG];
-#pragma unroll
-    for (int g = 0; g < NG; ++g) vsb[g] = vs_next[g];
-    if (more) load_codes();
-    const float kfac = p.scale_log2 * ks;
-    const bool ok = sb + lane < w1 && key_ok(sb + lane);
+    const float kfac = p.scale_log2 * ks * 16.f;
     float t[GP];
-    bool up = false;  // this lane's key passes a running maximum by 2^8, or a group's exponent
 #pragma unroll
-    for (int h = 0; h < GP; ++h) {
-      t[h] = ok ? s[h] * kfac : -INFINITY;
-      up |= t[h] > m_run[h] + 8.f;
-    }
+    for (int h = 0; h < GP; ++h) t[h] = fmaf(s[h], kfac, -m_use[h]);
+    const bool full = last >= 63 && (sb >= wlo || sb + 63 < wg);  // uniform: the query sees every key
+    const bool ok = lane <= last && (sb + lane >= wlo || sb + lane < wg);
+    if (!full) {
 #pragma unroll
-    for (int g = 0; g < NG; ++g) {
-      vsb[g] = ok ? vsb[g] & 0x7fffu : 0u;
-      up |= (int)(vsb[g] >> 7) > vexp[g];
+      for (int h = 0; h < GP; ++h) t[h] = ok ? t[h] : -INFINITY;
+#pragma unroll
+      for (int g = 0; g < NG; ++g) vs[g] = ok ? vs[g] : 0u;
     }
+    bool up = false;  // this lane's key passes a running maximum by 2^4, or a group's exponent
+#pragma unroll
+    for (int h = 0; h < GP; ++h) up |= t[h] > (m_run[h] == -INFINITY ? -INFINITY : 4.f);
+#pragma unroll
+    for (int g = 0; g < NG; ++g) up |= vs[g] > (uint32_t)(vexp[g] << 7 | 127);
     if (wave_ballot(up)) {  // uniform; the first block always
       float fa[4];
       {
         float alpha[GP];
 #pragma unroll
         for (int h = 0; h < GP; ++h) {
-          const float m_new = fmaxf(m_run[h], wave_max_dpp(t[h]));
+          const float x = full || ok ? s[h] * kfac : -INFINITY;
+          const float m_new = fmaxf(m_run[h], wave_max_dpp(x));
           alpha[h] = m_run[h] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run[h] - m_new);
           l_lane[h] *= alpha[h];
           m_run[h] = m_new;
+          m_use[h] = m_new == -INFINITY ? 0.f : m_new;
+          t[h] = x - m_use[h];
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) fa[i] = GP == 4 || !(lane & 16) ? alpha[i] : alpha[GP - 4 + i];
       }
 #pragma unroll
       for (int g = 0; g < NG; ++g) {
-        const int vnew = max(vexp[g], min((int)(wave_umax(vsb[g]) >> 7), 254));
-        const float f = vnew - vexp[g] > 126 ? 0.f : __uint_as_float((uint32_t)(127 + vexp[g] - vnew) << 23);
+        const int vnew = max(vexp[g], min((int)(wave_umax(vs[g] & 0x7fffu) >> 7), 254));
+        const float f = vnew - vexp[g] > 126 ? 0.f : pow2_field(127 + vexp[g] - vnew);
         vexp[g] = vnew;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -271,54 +320,71 @@ __global__ __launch_bounds__(kDecThreads, GP == 4 && D <= 128 ? 3 : GP == 8 && D
     float pj[GP];
 #pragma unroll
     for (int h = 0; h < GP; ++h) {
-      pj[h] = __builtin_amdgcn_exp2f(t[h] - (m_run[h] == -INFINITY ? 0.f : m_run[h]));
+      pj[h] = __builtin_amdgcn_exp2f(t[h]);
       l_lane[h] += pj[h];
     }
     // weights: [group][key][pieces 0 of the heads, pieces 1]
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
       if (g >= ng) break;
-      const float f = bf16_bits_to_f32(vsb[g]) * __uint_as_float((uint32_t)(259 - vexp[g]) << 23);
-      _Float16 w[2 * GP];
+      const float f = bf16_bits_to_f32(vs[g]) * pow2_field(264 - vexp[g] - odd4);
+      f16x8 w[GP / 4];
 #pragma unroll
       for (int h = 0; h < GP; ++h) {
         const float x = pj[h] * f;
-        w[h] = (_Float16)x;
-        w[GP + h] = (_Float16)(x - (float)w[h]);
+        const _Float16 x0 = (_Float16)x;
+        w[h / 8][h % 8] = x0;
+        w[(GP + h) / 8][(GP + h) % 8] = (_Float16)(x - (float)x0);
       }
 #pragma unroll
-      for (int i = 0; i < GP / 4; ++i) ((f16x8*)&pb[wave][g][lane][0])[i] = *(f16x8*)&w[8 * i];
+      for (int i = 0; i < GP / 4; ++i) ((f16x8*)&pb[wave][g][lane][0])[i] = w[i];
     }
+    // This block's value rows have arrived (and, issued after them, the next block's
+    // codes); they are read out before the next ones are sent into their place.
+    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    // P.V.  Lane l: operand row l % 16, keys 16 (l / 16) + 8 m + 0..7, in the
-    // nibbles' order 0 4 1 5 2 6 3 7.
-    const int r16 = lane & 15, key0 = lane & 48;
-    const int quarter = (r16 & 3) & (GP / 2 - 1);  // of the 2 GP rows (GP = 4: rows 8 to 15 repeat 0 to 7)
+    v2i nib[2 * NG];
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
       if (g >= ng) break;
-      f16x8 A[2];
+      nib[2 * g] = read_tr4(b_src[g]);
+      nib[2 * g + 1] = read_tr4(b_src[g] + 8);
+    }
+    __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    if (more) load_values(sb + 64, page_next);
+    // P.V.  Lane l: operand row l % 16, keys 16 (l / 16) + 8 m + 0..7, in the
+    // nibbles' order 0 4 1 5 2 6 3 7 (GP = 4: rows 8 to 15 repeat 0 to 7).
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      if (g >= ng) break;
 #pragma unroll
       for (int m = 0; m < 2; ++m) {
-        const int j = r16 >> 2;  // keys (j >> 1) + 4 (j & 1) for elements 0..3, and 2 more for 4..7
-        const _Float16* src = &pb[wave][g][key0 + 8 * m + (j >> 1) + 4 * (j & 1)][4 * quarter];
+        const _Float16* src = a_src + (g * 64 + 8 * m) * 2 * GP;
         const v4s lo = read_tr16(src), hi = read_tr16(src + 2 * 2 * GP);
-        A[m] = __builtin_bit_cast(f16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-      }
+        const f16x8 A = __builtin_bit_cast(f16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
-      for (int tt = 0; tt < 2; ++tt) {
-        const v2i n = read_tr4(vw + (key0 + r16) * PITCH + g * 16 + tt * 8);
-        acc[2 * g + tt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(A[0], nibbles_f16(n.x), acc[2 * g + tt], 0, 0, 0);
-        acc[2 * g + tt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(A[1], nibbles_f16(n.y), acc[2 * g + tt], 0, 0, 0);
+        for (int tt = 0; tt < 2; ++tt) {
+          floatx4 c = acc[2 * g + tt];
+          c = __builtin_amdgcn_mfma_f32_16x16x32_f16(A, nibbles_f16(nib[2 * g + tt][m]), c, 0, 0, 0);
+          acc[2 * g + tt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(A, __builtin_bit_cast(f16x8, minus8), c, 0, 0, 0);
+        }
       }
     }
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+    for (int c = 0; c < NKC; ++c) { ki[c] = ki2[c]; kq[c] = kq2[c]; }
+#pragma unroll
+    for (int g = 0; g < NG; ++g) vs[g] = vs2[g];
+    ks = ks2;
+    page = page_next;
   }
 
-  // The two pieces' sums, and the power of two of the weights.  Lane l, register i:
-  // row 4 (l / 16) + i, coordinate l % 16 of the tile.
+  // The two pieces' sums, and the powers of two of weights and numbers.  Lane l,
+  // register i: row 4 (l / 16) + i, coordinate l % 16 of the tile.
 #pragma unroll
   for (int h = 0; h < GP; ++h) l_lane[h] = wave_sum(l_lane[h]);
   __syncthreads();  // every wavefront is done with pb
@@ -328,7 +394,7 @@ __global__ __launch_bounds__(kDecThreads, GP == 4 && D <= 128 ? 3 : GP == 8 && D
   for (int t = 0; t < 2 * NG; ++t)
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      acc[t][i] = (acc[t][i] + __shfl_xor(acc[t][i], 4 * GP, 64)) * __uint_as_float((uint32_t)(vexp[t / 2] - 5) << 23);
+      acc[t][i] = (acc[t][i] + __shfl_xor(acc[t][i], 4 * GP, 64)) * pow2_field(vexp[t / 2] - 10) * 0x1p24f;
   if (lane < 4 * GP) {
     const int h0 = GP == 4 ? 0 : 4 * (lane >> 4);
 #pragma unroll
@@ -394,16 +460,20 @@ __global__ __launch_bounds__(kMergeQ4) void sfa_decode_q4_combine_kernel(DecPara
 template <int D, int GP, int KC8>
 void launch_q4_t(const DecParams& p, const DecodeArgs& a, hipStream_t stream) {
   const dim3 grid = p.by_slot ? dim3(a.B * p.Hkv, p.nch) : dim3(p.nch, a.B * p.Hkv), block(kDecThreads);
-  if (p.table)
-    hipLaunchKernelGGL((sfa_decode_q4_kernel<D, GP, KC8, true>), grid, block, 0, stream, p, a.d, a.v_scale16);
-  else
-    hipLaunchKernelGGL((sfa_decode_q4_kernel<D, GP, KC8, false>), grid, block, 0, stream, p, a.d, a.v_scale16);
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, p, a.d, a.v_scale16); };
+  if (!p.table) go(sfa_decode_q4_kernel<D, GP, KC8, 0>);
+  else if (p.log2P >= 6) go(sfa_decode_q4_kernel<D, GP, KC8, 1>);
+  else go(sfa_decode_q4_kernel<D, GP, KC8, 2>);
 }
 
 template <int D, int GP>
 void launch_q4_k(const DecParams& p, const DecodeArgs& a, hipStream_t stream) {
-  if (D < 256 && a.k == 16) launch_q4_t<D, GP, 2>(p, a, stream);
-  else launch_q4_t<D, GP, 0>(p, a, stream);
+  if constexpr (D < 256) {
+    if (a.k == 8) return launch_q4_t<D, GP, 1>(p, a, stream);
+    if (a.k == 16) return launch_q4_t<D, GP, 2>(p, a, stream);
+    if (a.k == 32) return launch_q4_t<D, GP, 4>(p, a, stream);
+  }
+  launch_q4_t<D, GP, 0>(p, a, stream);
 }
 
 template <int D>
