@@ -21,9 +21,10 @@
 //            the 8 off again, block by block, so that the sums stay small.
 // Both operands have 16 or 8 keys of one row in a lane, and both are held key by
 // key: the transposing LDS reads turn them, ds_read_b64_tr_b4 the cached nibbles
-// as they are and ds_read_b64_tr_b16 the weights.  Value rows go to LDS directly
-// (global_load_lds), one block of keys ahead, the 16-byte pieces of a row exchanged
-// so that the transposing reads find each key on banks of its own.
+// as they are and ds_read_b64_tr_b16 the weights.  Value rows are loaded a block of
+// keys ahead and written to LDS with the 16-byte pieces of a row exchanged, so that the
+// transposing reads find each key on banks of its own.  (Through registers: with
+// loads sent to LDS directly, the compiler waits for them at every later LDS read.)
 //
 // float16 range: each group's weights are scaled by a power of two that follows
 // the largest value scale seen in the group, as the running maximum does for p
@@ -164,41 +165,47 @@ void sfa_decode_q4_kernel(DecParams p, int dd, const uint16_t* vscale) {
     else return kv_row0 + sb;
   };
 
-  // Value rows, to LDS directly: 16-byte piece x of the block's 64 ng, x = lane + 64 i,
+  // Value rows: 16-byte piece x of the block's 64 ng, x = lane + 64 i,
   // belongs to key x / ng and holds its piece (x % ng) ^ ((key / (16 / ng)) % ng) (ng a
   // power of two; the others keep their order).
   unsigned char* vw = vt[wave];
   const int sw_mask = (ng & (ng - 1)) == 0 ? ng - 1 : 0;
   const int sw_shift = ng >= 8 ? 1 : ng >= 4 ? 2 : ng >= 2 ? 3 : 4;
   const uint8_t* vc = (const uint8_t*)p.v;
+  const uint32_t run_off = (lane / NG) * (D / 2) + (((lane % NG) ^ ((lane / NG >> sw_shift) & sw_mask)) * 16);
+  u32x4 vreg[NG];
   auto load_values = [&](int sb, int page) {  // page: of this lane's key (PG 2)
     const int last = w1 - 1 - sb;
     const uint8_t* base = PG < 2 ? vc + block_row(sb) * (d / 2) : nullptr;
+    if constexpr (PG < 2 && D <= 128) {
+      if (last >= 63) {  // a whole block: its rows are one run
+#pragma unroll
+        for (int i = 0; i < NG; ++i) vreg[i] = *(const u32x4*)(base + run_off + i * 1024);
+        return;
+      }
+    }
 #pragma unroll
     for (int i = 0; i < NG; ++i) {
       if (i >= ng) break;
-      const int x = lane + 64 * i, key = x / ng;
+      const int x = lane + 64 * i, key = x / ng, kc = min(key, last);
       const int piece = (x - key * ng) ^ ((key >> sw_shift) & sw_mask);
-      const uint8_t* src;
-      if constexpr (PG < 2) {
-        src = base + (uint32_t)((last >= 63 ? key : min(key, last)) * (d / 2) + piece * 16);
-      } else {
-        const int kc = min(key, last);
-        src = vc + paged_row(__shfl(page, kc, 64), sb + kc) * (d / 2) + piece * 16;
-      }
-      __builtin_amdgcn_global_load_lds(src, (__attribute__((address_space(3))) void*)(vw + i * 1024), 16, 0, 0);
+      if constexpr (PG < 2)
+        vreg[i] = *(const u32x4*)(base + (uint32_t)(kc * (d / 2) + piece * 16));
+      else
+        vreg[i] = *(const u32x4*)(vc + paged_row(__shfl(page, kc, 64), sb + kc) * (d / 2) + piece * 16);
     }
   };
   // A key's codes and scales (lane = key), loaded a block ahead.
   constexpr int NKC = KC8 > 0 ? KC8 : 1;
   uint2 ki[NKC], ki2[NKC];
-  uint32_t kq[NKC], kq2[NKC], vs[NG], vs2[NG];
+  constexpr int NVS = D <= 128 ? NG / 2 : NG;  // value scales, two to a word where a row has 2 or 4
+  uint32_t kq[NKC], kq2[NKC], vraw[NVS], vraw2[NVS];
   float ks = 0.f, ks2 = 0.f;
   auto lane_row = [&](int sb, int page) -> int64_t {
     const int kc = min(lane, w1 - 1 - sb);
     return PG < 2 ? block_row(sb) + kc : paged_row(page, sb + kc);
   };
-  auto load_codes = [&](int sb, int page, uint2 (&ki)[NKC], uint32_t (&kq)[NKC], float& ks, uint32_t (&vs)[NG]) {
+  auto load_codes = [&](int sb, int page, uint2 (&ki)[NKC], uint32_t (&kq)[NKC], float& ks, uint32_t (&vr)[NVS]) {
     const int64_t row = PG < 2 ? block_row(sb) : lane_row(sb, page);
     const uint32_t o = PG < 2 ? (uint32_t)min(lane, w1 - 1 - sb) : 0u;
     if constexpr (KC8 > 0) {
@@ -214,20 +221,19 @@ void sfa_decode_q4_kernel(DecParams p, int dd, const uint16_t* vscale) {
     const uint16_t* pv = vscale + row * ng + o * ng;
     if constexpr (D == 128) {
       const uint2 w = *(const uint2*)pv;
-      vs[0] = w.x & 0xffffu; vs[1] = w.x >> 16; vs[2] = w.y & 0xffffu; vs[3] = w.y >> 16;
+      vr[0] = w.x; vr[1] = w.y;
     } else if constexpr (D == 64) {
-      const uint32_t w = *(const uint32_t*)pv;
-      vs[0] = w & 0xffffu; vs[1] = w >> 16;
+      vr[0] = *(const uint32_t*)pv;
     } else {
 #pragma unroll
-      for (int g = 0; g < NG; ++g) vs[g] = g < ng ? pv[g] : 0;
+      for (int g = 0; g < NG; ++g) vr[g] = g < ng ? pv[g] : 0;
     }
   };
   auto page_of = [&](int sb) -> int {
     if constexpr (PG == 2) return __shfl(tblv, (min(sb + lane, w1 - 1) >> p.log2P) - pg0, 64);
     else return 0;
   };
-  // operand addresses in LDS (see the P.V loop)
+  // operand addresses in LDS
   const int r16 = lane & 15, key0 = lane & 48;
   const _Float16* a_src = &pb[wave][0][key0 + (r16 >> 3) + 4 * ((r16 >> 2) & 1)][4 * ((r16 & 3) & (GP / 2 - 1))];
   const unsigned char* b_src[NG];
@@ -240,14 +246,20 @@ void sfa_decode_q4_kernel(DecParams p, int dd, const uint16_t* vscale) {
   int page = 0;
   if (w0 < w1) {
     page = page_of(w0);
-    load_codes(w0, page, ki, kq, ks, vs);
+    load_codes(w0, page, ki, kq, ks, vraw);
     load_values(w0, page);
   }
   for (int sb = w0; sb < w1; sb += 64) {
     const int last = w1 - 1 - sb;
     const bool more = last >= 64;
     const int page_next = more ? page_of(sb + 64) : 0;
-    if (more) load_codes(sb + 64, page_next, ki2, kq2, ks2, vs2);
+#pragma unroll
+    for (int i = 0; i < NG; ++i)
+      if (i < ng) *(u32x4*)(vw + (lane + 64 * i) * 16) = vreg[i];
+    if (more) {
+      load_codes(sb + 64, page_next, ki2, kq2, ks2, vraw2);
+      load_values(sb + 64, page_next);
+    }
     // scores: the code values count in sixteenths (v_cvt_off_f32_i4)
     float s[GP];
 #pragma unroll
@@ -272,6 +284,9 @@ void sfa_decode_q4_kernel(DecParams p, int dd, const uint16_t* vscale) {
                ((const uint32_t*)((const uint8_t*)p.kc_val + row * (k / 2)))[c]);
     }
     const float kfac = p.scale_log2 * ks * 16.f;
+    uint32_t vs[NG];
+#pragma unroll
+    for (int g = 0; g < NG; ++g) vs[g] = D > 128 ? vraw[g % NVS] : (g & 1) ? vraw[g / 2] >> 16 : vraw[g / 2] & 0xffffu;
     float t[GP];
 #pragma unroll
     for (int h = 0; h < GP; ++h) t[h] = fmaf(s[h], kfac, -m_use[h]);
@@ -339,27 +354,15 @@ void sfa_decode_q4_kernel(DecParams p, int dd, const uint16_t* vscale) {
 #pragma unroll
       for (int i = 0; i < GP / 4; ++i) ((f16x8*)&pb[wave][g][lane][0])[i] = w[i];
     }
-    // This block's value rows have arrived (and, issued after them, the next block's
-    // codes); they are read out before the next ones are sent into their place.
-    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    v2i nib[2 * NG];
+    // P.V.
+    // Lane l: operand row l % 16, keys 16 (l / 16) + 8 m + 0..7, in the nibbles' order
+    // 0 4 1 5 2 6 3 7 (GP = 4: weight rows 8 to 15 repeat 0 to 7).
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
       if (g >= ng) break;
-      nib[2 * g] = read_tr4(b_src[g]);
-      nib[2 * g + 1] = read_tr4(b_src[g] + 8);
-    }
-    __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    if (more) load_values(sb + 64, page_next);
-    // P.V.  Lane l: operand row l % 16, keys 16 (l / 16) + 8 m + 0..7, in the
-    // nibbles' order 0 4 1 5 2 6 3 7 (GP = 4: rows 8 to 15 repeat 0 to 7).
-#pragma unroll
-    for (int g = 0; g < NG; ++g) {
-      if (g >= ng) break;
+      const v2i nib[2] = {read_tr4(b_src[g]), read_tr4(b_src[g] + 8)};
 #pragma unroll
       for (int m = 0; m < 2; ++m) {
         const _Float16* src = a_src + (g * 64 + 8 * m) * 2 * GP;
@@ -368,7 +371,7 @@ void sfa_decode_q4_kernel(DecParams p, int dd, const uint16_t* vscale) {
 #pragma unroll
         for (int tt = 0; tt < 2; ++tt) {
           floatx4 c = acc[2 * g + tt];
-          c = __builtin_amdgcn_mfma_f32_16x16x32_f16(A, nibbles_f16(nib[2 * g + tt][m]), c, 0, 0, 0);
+          c = __builtin_amdgcn_mfma_f32_16x16x32_f16(A, nibbles_f16(nib[tt][m]), c, 0, 0, 0);
           acc[2 * g + tt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(A, __builtin_bit_cast(f16x8, minus8), c, 0, 0, 0);
         }
       }
@@ -378,7 +381,7 @@ void sfa_decode_q4_kernel(DecParams p, int dd, const uint16_t* vscale) {
 #pragma unroll
     for (int c = 0; c < NKC; ++c) { ki[c] = ki2[c]; kq[c] = kq2[c]; }
 #pragma unroll
-    for (int g = 0; g < NG; ++g) vs[g] = vs2[g];
+    for (int g = 0; g < NVS; ++g) vraw[g] = vraw2[g];
     ks = ks2;
     page = page_next;
   }
