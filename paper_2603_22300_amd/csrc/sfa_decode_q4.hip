@@ -63,7 +63,7 @@ __device__ __forceinline__ float pow2_field(int field) { return __uint_as_float(
 // PG: 0 contiguous, 1 pages of 64 positions or more (a block of keys has one), 2
 // pages of 16 or 32.
 template <int D, int GP, int KC8, int PG>
-__global__ __launch_bounds__(kDecThreads, GP == 4 && D <= 128 ? 3 : GP == 8 && D <= 128 ? 2 : 1)
+__global__ __launch_bounds__(kDecThreads, GP == 4 && D <= 128 ? 4 : GP == 8 && D <= 128 ? 2 : 1)
 void sfa_decode_q4_kernel(DecParams p, int dd, const uint16_t* vscale) {
   constexpr int NG = D / 32;  // value scale groups, two 16-coordinate tiles each
   const int d = D == 256 ? dd : D, ng = d / 32;
@@ -132,8 +132,11 @@ void sfa_decode_q4_kernel(DecParams p, int dd, const uint16_t* vscale) {
   // 2^10 to 2^11 and a weight at most 2^15, and the smallest weight that the second
   // piece still holds is 2^-34 of p = 1 (2^-30 for odd keys).
   int vexp[NG];
+  float vpow[NG];  // that power of two, this lane's key's
+  const int odd4 = 4 * (lane & 1);
 #pragma unroll
-  for (int g = 0; g < NG; ++g) vexp[g] = 11;
+  for (int g = 0; g < NG; ++g) { vexp[g] = 11; vpow[g] = pow2_field(264 - 11 - odd4); }
+  float pass = -INFINITY;  // exponents past it raise the maxima: 2^4 once there are any
 
   const int64_t kv_row0 = ((int64_t)b * p.Hkv + hkv) * p.Lmax;
   const int per_wave = plan.c / kDecWaves;
@@ -197,15 +200,15 @@ void sfa_decode_q4_kernel(DecParams p, int dd, const uint16_t* vscale) {
   };
   // A key's codes and scales (lane = key), loaded a block ahead.
   constexpr int NKC = KC8 > 0 ? KC8 : 1;
-  uint2 ki[NKC], ki2[NKC];
+  uint2 ki[NKC];
   constexpr int NVS = D <= 128 ? NG / 2 : NG;  // value scales, two to a word where a row has 2 or 4
-  uint32_t kq[NKC], kq2[NKC], vraw[NVS], vraw2[NVS];
-  float ks = 0.f, ks2 = 0.f;
+  uint32_t kq[NKC], vraw[NVS];
+  float ks = 0.f;
   auto lane_row = [&](int sb, int page) -> int64_t {
     const int kc = min(lane, w1 - 1 - sb);
     return PG < 2 ? block_row(sb) + kc : paged_row(page, sb + kc);
   };
-  auto load_codes = [&](int sb, int page, uint2 (&ki)[NKC], uint32_t (&kq)[NKC], float& ks, uint32_t (&vr)[NVS]) {
+  auto load_codes = [&](int sb, int page) {
     const int64_t row = PG < 2 ? block_row(sb) : lane_row(sb, page);
     const uint32_t o = PG < 2 ? (uint32_t)min(lane, w1 - 1 - sb) : 0u;
     if constexpr (KC8 > 0) {
@@ -221,12 +224,12 @@ void sfa_decode_q4_kernel(DecParams p, int dd, const uint16_t* vscale) {
     const uint16_t* pv = vscale + row * ng + o * ng;
     if constexpr (D == 128) {
       const uint2 w = *(const uint2*)pv;
-      vr[0] = w.x; vr[1] = w.y;
+      vraw[0] = w.x; vraw[1] = w.y;
     } else if constexpr (D == 64) {
-      vr[0] = *(const uint32_t*)pv;
+      vraw[0] = *(const uint32_t*)pv;
     } else {
 #pragma unroll
-      for (int g = 0; g < NG; ++g) vr[g] = g < ng ? pv[g] : 0;
+      for (int g = 0; g < NG; ++g) vraw[g] = g < ng ? pv[g] : 0;
     }
   };
   auto page_of = [&](int sb) -> int {
@@ -241,25 +244,21 @@ void sfa_decode_q4_kernel(DecParams p, int dd, const uint16_t* vscale) {
   for (int g = 0; g < NG; ++g)
     b_src[g] = vw + (key0 + r16) * (d / 2) + (g ^ ((r16 >> sw_shift) & sw_mask)) * 16;
   const u32x4 minus8 = {0x80088008u, 0x80808080u, 0x80088008u, 0x80808080u};
-  const int odd4 = 4 * (lane & 1);
 
   int page = 0;
   if (w0 < w1) {
     page = page_of(w0);
-    load_codes(w0, page, ki, kq, ks, vraw);
+    load_codes(w0, page);
     load_values(w0, page);
   }
   for (int sb = w0; sb < w1; sb += 64) {
     const int last = w1 - 1 - sb;
-    const bool more = last >= 64;
-    const int page_next = more ? page_of(sb + 64) : 0;
+    const int sb_next = last >= 64 ? sb + 64 : sb;  // (the last block loads itself again, unused)
+    const int page_next = page_of(sb_next);
 #pragma unroll
     for (int i = 0; i < NG; ++i)
       if (i < ng) *(u32x4*)(vw + (lane + 64 * i) * 16) = vreg[i];
-    if (more) {
-      load_codes(sb + 64, page_next, ki2, kq2, ks2, vraw2);
-      load_values(sb + 64, page_next);
-    }
+    load_values(sb_next, page_next);
     // scores: the code values count in sixteenths (v_cvt_off_f32_i4)
     float s[GP];
 #pragma unroll
@@ -276,7 +275,12 @@ void sfa_decode_q4_kernel(DecParams p, int dd, const uint16_t* vscale) {
     };
     if constexpr (KC8 > 0) {
 #pragma unroll
-      for (int c = 0; c < KC8; ++c) score8(ki[c], kq[c]);
+      for (int c = 0; c < KC8; ++c) {
+        score8(ki[c], kq[c]);
+        // eight gathers in flight, not all of them: registers
+#pragma unroll
+        for (int h = 0; h < GP; ++h) asm volatile("" : "+v"(s[h]));
+      }
     } else {
       const int64_t row = lane_row(sb, page);
       for (int c = 0; c < k / 8; ++c)
@@ -284,9 +288,11 @@ void sfa_decode_q4_kernel(DecParams p, int dd, const uint16_t* vscale) {
                ((const uint32_t*)((const uint8_t*)p.kc_val + row * (k / 2)))[c]);
     }
     const float kfac = p.scale_log2 * ks * 16.f;
-    uint32_t vs[NG];
+    uint32_t vs[NG];  // the value scales, as float32 bits
 #pragma unroll
-    for (int g = 0; g < NG; ++g) vs[g] = D > 128 ? vraw[g % NVS] : (g & 1) ? vraw[g / 2] >> 16 : vraw[g / 2] & 0xffffu;
+    for (int g = 0; g < NG; ++g)
+      vs[g] = D > 128 ? vraw[g % NVS] << 16 : (g & 1) ? vraw[g / 2] & 0xffff0000u : vraw[g / 2] << 16;
+    load_codes(sb_next, page_next);
     float t[GP];
 #pragma unroll
     for (int h = 0; h < GP; ++h) t[h] = fmaf(s[h], kfac, -m_use[h]);
@@ -298,12 +304,14 @@ void sfa_decode_q4_kernel(DecParams p, int dd, const uint16_t* vscale) {
 #pragma unroll
       for (int g = 0; g < NG; ++g) vs[g] = ok ? vs[g] : 0u;
     }
-    bool up = false;  // this lane's key passes a running maximum by 2^4, or a group's exponent
+    // a key that passes a running maximum by 2^4, or a group's exponent
+    float tmax = t[0];
 #pragma unroll
-    for (int h = 0; h < GP; ++h) up |= t[h] > (m_run[h] == -INFINITY ? -INFINITY : 4.f);
+    for (int h = 1; h < GP; ++h) tmax = fmaxf(tmax, t[h]);
+    uint64_t up = wave_ballot(tmax > pass);
 #pragma unroll
-    for (int g = 0; g < NG; ++g) up |= vs[g] > (uint32_t)(vexp[g] << 7 | 127);
-    if (wave_ballot(up)) {  // uniform; the first block always
+    for (int g = 0; g < NG; ++g) up |= wave_ballot(vs[g] > (uint32_t)(vexp[g] << 23 | 0x7fffff));
+    if (up) {  // uniform; the first block always
       float fa[4];
       {
         float alpha[GP];
@@ -317,14 +325,16 @@ void sfa_decode_q4_kernel(DecParams p, int dd, const uint16_t* vscale) {
           m_use[h] = m_new == -INFINITY ? 0.f : m_new;
           t[h] = x - m_use[h];
         }
+        pass = m_run[0] == -INFINITY ? -INFINITY : 4.f;
 #pragma unroll
         for (int i = 0; i < 4; ++i) fa[i] = GP == 4 || !(lane & 16) ? alpha[i] : alpha[GP - 4 + i];
       }
 #pragma unroll
       for (int g = 0; g < NG; ++g) {
-        const int vnew = max(vexp[g], min((int)(wave_umax(vs[g] & 0x7fffu) >> 7), 254));
+        const int vnew = max(vexp[g], min((int)(wave_umax(vs[g] & 0x7fffffffu) >> 23), 254));
         const float f = vnew - vexp[g] > 126 ? 0.f : pow2_field(127 + vexp[g] - vnew);
         vexp[g] = vnew;
+        vpow[g] = pow2_field(264 - vnew - odd4);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           acc[2 * g][i] *= f * fa[i];
@@ -342,20 +352,22 @@ void sfa_decode_q4_kernel(DecParams p, int dd, const uint16_t* vscale) {
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
       if (g >= ng) break;
-      const float f = bf16_bits_to_f32(vs[g]) * pow2_field(264 - vexp[g] - odd4);
+      const float f = __uint_as_float(vs[g]) * vpow[g];
       f16x8 w[GP / 4];
 #pragma unroll
-      for (int h = 0; h < GP; ++h) {
-        const float x = pj[h] * f;
-        const _Float16 x0 = (_Float16)x;
-        w[h / 8][h % 8] = x0;
-        w[(GP + h) / 8][(GP + h) % 8] = (_Float16)(x - (float)x0);
+      for (int h = 0; h < GP; h += 2) {
+        const auto x0 = __builtin_amdgcn_cvt_pkrtz(pj[h] * f, pj[h + 1] * f);
+        w[h / 8][h % 8] = (_Float16)x0[0];
+        w[h / 8][h % 8 + 1] = (_Float16)x0[1];
+        w[(GP + h) / 8][(GP + h) % 8] = (_Float16)fmaf(pj[h], f, -(float)x0[0]);
+        w[(GP + h) / 8][(GP + h) % 8 + 1] = (_Float16)fmaf(pj[h + 1], f, -(float)x0[1]);
       }
 #pragma unroll
       for (int i = 0; i < GP / 4; ++i) ((f16x8*)&pb[wave][g][lane][0])[i] = w[i];
     }
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_sched_barrier(0);
     // P.V.
     // Lane l: operand row l % 16, keys 16 (l / 16) + 8 m + 0..7, in the nibbles' order
     // 0 4 1 5 2 6 3 7 (GP = 4: weight rows 8 to 15 repeat 0 to 7).
@@ -378,32 +390,22 @@ void sfa_decode_q4_kernel(DecParams p, int dd, const uint16_t* vscale) {
     }
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-#pragma unroll
-    for (int c = 0; c < NKC; ++c) { ki[c] = ki2[c]; kq[c] = kq2[c]; }
-#pragma unroll
-    for (int g = 0; g < NVS; ++g) vraw[g] = vraw2[g];
-    ks = ks2;
     page = page_next;
   }
 
-  // The two pieces' sums, and the powers of two of weights and numbers.  Lane l,
-  // register i: row 4 (l / 16) + i, coordinate l % 16 of the tile.
+  // Both pieces' sums to LDS, with the powers of two of weights and numbers taken out
+  // (2^(137 - vexp) 2^-24).  Lane l, register i: row 4 (l / 16) + i, coordinate l % 16.
 #pragma unroll
   for (int h = 0; h < GP; ++h) l_lane[h] = wave_sum(l_lane[h]);
   __syncthreads();  // every wavefront is done with pb
-  float* red_o = (float*)&pb[0][0][0][0];  // [wave][GP][D]
-  static_assert(sizeof(pb) >= sizeof(float) * kDecWaves * GP * D, "the partials fit the weights' place");
-#pragma unroll
-  for (int t = 0; t < 2 * NG; ++t)
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      acc[t][i] = (acc[t][i] + __shfl_xor(acc[t][i], 4 * GP, 64)) * pow2_field(vexp[t / 2] - 10) * 0x1p24f;
-  if (lane < 4 * GP) {
-    const int h0 = GP == 4 ? 0 : 4 * (lane >> 4);
+  float* red_o = (float*)&pb[0][0][0][0];  // [wave][2 GP][D]
+  static_assert(sizeof(pb) >= sizeof(float) * kDecWaves * 2 * GP * D, "the partials fit the weights' place");
+  if (GP == 8 || lane < 32) {
+    float* dst = red_o + (wave * 2 * GP + 4 * (lane >> 4)) * D + (lane & 15);
 #pragma unroll
     for (int t = 0; t < 2 * NG; ++t)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) red_o[(wave * GP + h0 + i) * D + 16 * t + (lane & 15)] = acc[t][i];
+      for (int i = 0; i < 4; ++i) dst[i * D + 16 * t] = ldexpf(acc[t][i], vexp[t / 2] - 113);
   }
   if (lane == 0) {
 #pragma unroll
@@ -419,9 +421,9 @@ void sfa_decode_q4_kernel(DecParams p, int dd, const uint16_t* vscale) {
     float lsum = 0.f, osum = 0.f;
 #pragma unroll
     for (int w = 0; w < kDecWaves; ++w) {
-      const float sc = exp2f(red_m[w][h] - Mu);
+      const float sc = __builtin_amdgcn_exp2f(red_m[w][h] - Mu);
       lsum += sc * red_l[w][h];
-      osum += sc * red_o[(w * GP + h) * D + c];
+      osum += sc * (red_o[(w * 2 * GP + h) * D + c] + red_o[(w * 2 * GP + GP + h) * D + c]);
     }
     const int64_t part = ((int64_t)b * p.Hq + hkv * p.G + h) * p.nch + slot;
     p.ws_o[part * d + c] = osum;
