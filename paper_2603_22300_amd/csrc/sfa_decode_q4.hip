@@ -58,6 +58,20 @@ __device__ __forceinline__ f16x8 nibbles_f16(uint32_t x) {
 
 __device__ __forceinline__ float pow2_field(int field) { return __uint_as_float((uint32_t)field << 23); }
 
+// Sum over the wavefront in every lane, by DPP steps and four readlanes.
+template <int CTRL>
+__device__ __forceinline__ float dpp_add_step(float v) {
+  return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, false));
+}
+__device__ __forceinline__ float wave_sum_dpp(float x) {
+  x = dpp_add_step<0xb1>(x);   // quad_perm 1,0,3,2
+  x = dpp_add_step<0x4e>(x);   // quad_perm 2,3,0,1
+  x = dpp_add_step<0x141>(x);  // row_half_mirror
+  x = dpp_add_step<0x140>(x);  // row_mirror
+  auto row = [&](int l) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), l)); };
+  return (row(0) + row(16)) + (row(32) + row(48));
+}
+
 // D: head dimension, or 256 for any d <= 256 (dd then counts).  GP: query heads
 // per KV head rounded up to 4 or 8.  KC8: k / 8, or 0 to take it from p.k.
 // PG: 0 contiguous, 1 pages of 64 positions or more (a block of keys has one), 2
@@ -81,6 +95,18 @@ void sfa_decode_q4_kernel(DecParams p, int dd, const uint16_t* vscale) {
   if (!by_slot && gridDim.x % 2 == 0) slot_u = (slot_u + (unsigned)bh + ((unsigned)bh >> 2)) % gridDim.x;
   const int slot = (int)slot_u;
   const int b = bh / p.Hkv, hkv = bh - b * p.Hkv;
+  // The query rows this wavefront will code are read beside the length, and the first
+  // block of keys before they are coded: a step of few keys is this chain of loads.
+  constexpr int E = (D + 63) / 64, QH = GP / kDecWaves;
+  uint32_t qbits[QH][E];
+  if (p.q_dense) {
+#pragma unroll
+    for (int j = 0; j < QH; ++j) {
+      const float* qr = p.q_dense + ((int64_t)b * p.Hq + hkv * p.G + min(wave + kDecWaves * j, p.G - 1)) * d;
+#pragma unroll
+      for (int e = 0; e < E; ++e) qbits[j][e] = __float_as_uint(qr[min(lane + 64 * e, d - 1)]);
+    }
+  }
   const int L = seq_len_of(p.seq_len, b, p.Lmax);
   const DecPlan plan = decode_plan(L, p.window, p.n_global, p.aim);
   if (slot >= plan.count) return;
@@ -90,36 +116,6 @@ void sfa_decode_q4_kernel(DecParams p, int dd, const uint16_t* vscale) {
   if (winq && chunk >= plan.ngc) chunk += plan.wc0 - plan.ngc;
   const int c0 = chunk * plan.c;
   const int c1 = min(L, c0 + plan.c);
-
-  // dense query rows
-  for (int x = tid; x < 256 * GP; x += kDecThreads) (&qd[0][0])[x] = 0.f;
-  __syncthreads();
-  if (p.q_dense) {
-    constexpr int E = (D + 63) / 64;
-    for (int h = wave; h < p.G; h += kDecWaves) {
-      const float* qr = p.q_dense + ((int64_t)b * p.Hq + hkv * p.G + h) * d;
-      uint32_t bits[E], key[E];
-      bool sel[E];
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const int c = lane + 64 * e;
-        bits[e] = __float_as_uint(qr[min(c, d - 1)]);
-        key[e] = topk_key(bits[e], c < d);
-      }
-      topk_select<E>(key, k, sel);
-#pragma unroll
-      for (int e = 0; e < E; ++e)
-        if (sel[e] && lane + 64 * e < d) qd[lane + 64 * e][h] = __uint_as_float(bits[e]);
-    }
-  } else {
-    for (int x = tid; x < p.G * k; x += kDecThreads) {
-      const int h = x / k, t = x - h * k;
-      const int64_t qi = ((int64_t)b * p.Hq + hkv * p.G + h) * k + t;
-      const int u = min(load_idx(p.q_idx, qi, p.qifmt, 255), d - 1);
-      qd[u][h] = load_val(p.q_val, qi, p.qvfmt);
-    }
-  }
-  __syncthreads();
 
   float m_run[GP], m_use[GP], l_lane[GP];  // m_use: m_run, or 0 before the first key
 #pragma unroll
@@ -251,6 +247,32 @@ void sfa_decode_q4_kernel(DecParams p, int dd, const uint16_t* vscale) {
     load_codes(w0, page);
     load_values(w0, page);
   }
+
+  // dense query rows
+  for (int x = tid; x < 256 * GP; x += kDecThreads) (&qd[0][0])[x] = 0.f;
+  __syncthreads();
+  if (p.q_dense) {
+#pragma unroll
+    for (int j = 0; j < QH; ++j) {
+      const int h = wave + kDecWaves * j;
+      uint32_t key[E];
+      bool sel[E];
+#pragma unroll
+      for (int e = 0; e < E; ++e) key[e] = topk_key(qbits[j][e], lane + 64 * e < d);
+      topk_select<E>(key, k, sel);
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        if (h < p.G && sel[e] && lane + 64 * e < d) qd[lane + 64 * e][h] = __uint_as_float(qbits[j][e]);
+    }
+  } else {
+    for (int x = tid; x < p.G * k; x += kDecThreads) {
+      const int h = x / k, t = x - h * k;
+      const int64_t qi = ((int64_t)b * p.Hq + hkv * p.G + h) * k + t;
+      const int u = min(load_idx(p.q_idx, qi, p.qifmt, 255), d - 1);
+      qd[u][h] = load_val(p.q_val, qi, p.qvfmt);
+    }
+  }
+  __syncthreads();
   for (int sb = w0; sb < w1; sb += 64) {
     const int last = w1 - 1 - sb;
     const int sb_next = last >= 64 ? sb + 64 : sb;  // (the last block loads itself again, unused)
@@ -396,7 +418,7 @@ void sfa_decode_q4_kernel(DecParams p, int dd, const uint16_t* vscale) {
   // Both pieces' sums to LDS, with the powers of two of weights and numbers taken out
   // (2^(137 - vexp) 2^-24).  Lane l, register i: row 4 (l / 16) + i, coordinate l % 16.
 #pragma unroll
-  for (int h = 0; h < GP; ++h) l_lane[h] = wave_sum(l_lane[h]);
+  for (int h = 0; h < GP; ++h) l_lane[h] = wave_sum_dpp(l_lane[h]);
   __syncthreads();  // every wavefront is done with pb
   float* red_o = (float*)&pb[0][0][0][0];  // [wave][2 GP][D]
   static_assert(sizeof(pb) >= sizeof(float) * kDecWaves * 2 * GP * D, "the partials fit the weights' place");
@@ -431,35 +453,99 @@ void sfa_decode_q4_kernel(DecParams p, int dd, const uint16_t* vscale) {
   }
 }
 
-// Merge of the chunks' partials, one workgroup per query head: thread groups of d
-// over the chunks, in a fixed order (as sfa_decode_combine_kernel, for any d).
-constexpr int kMergeQ4 = 512;
-__global__ __launch_bounds__(kMergeQ4) void sfa_decode_q4_combine_kernel(DecParams p, int d, int groups, void* o,
-                                                                         int obf16, float* lse) {
-  __shared__ float part[kMergeQ4];
-  const int bh = blockIdx.x, b = bh / p.Hq;
-  const int grp = threadIdx.x / d, dd = threadIdx.x - grp * d, lane = threadIdx.x & 63;
-  const int L = seq_len_of(p.seq_len, b, p.Lmax);
-  const int nc = decode_plan(L, p.window, p.n_global, p.aim).count;
+// Merge of the chunks' partials by their LSE.  A wavefront holds a query head's row,
+// lane l coordinates l + 64 i.  The output is kMergeQ4 sums, each over the chunks of
+// one residue in order, added in order: by as many wavefronts (WIDE), or in turn by
+// one.  Which of the two runs follows the cache's capacity; the sums, and so the bits,
+// do not.  A chain of dependent loads is what this kernel's time is made of: the first
+// maxima, sums and rows are read beside the length, before it is known how many of
+// them count (slots past them exist, unwritten).
+constexpr int kMergeQ4 = 8;
+template <int NV, bool WIDE>
+__global__ __launch_bounds__(WIDE ? 64 * kMergeQ4 : 256) void sfa_decode_q4_combine_kernel(DecParams p, int rows, int d,
+                                                                                        void* o, int obf16, float* lse) {
+  constexpr int NS = WIDE ? 1 : kMergeQ4;  // sums in this wavefront
+  __shared__ float part[WIDE ? kMergeQ4 : 1][64 * NV];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int bh = WIDE ? (int)blockIdx.x : (int)blockIdx.x * 4 + wave;
+  if (bh >= rows) return;  // uniform per wave; no workgroup barrier in this form
   const int64_t s0 = (int64_t)bh * p.nch;
-  float M = -INFINITY;
-  for (int c = lane; c < nc; c += 64) M = fmaxf(M, p.ws_m[s0 + c]);
-  M = wave_max(M);
+  const int at = min(lane, p.nch - 1);
+  const float m0 = p.ws_m[s0 + at], l0 = p.ws_l[s0 + at];
+  float x[NS][NV];
+  auto load_rows = [&](int c0) {
+#pragma unroll
+    for (int g = 0; g < NS; ++g) {
+      const float* src = p.ws_o + (s0 + min(c0 + (WIDE ? wave : g), p.nch - 1)) * d;
+#pragma unroll
+      for (int i = 0; i < NV; ++i) x[g][i] = src[min(lane + 64 * i, d - 1)];
+    }
+  };
+  load_rows(0);
+  const int L = seq_len_of(p.seq_len, bh / p.Hq, p.Lmax);
+  const int nc = decode_plan(L, p.window, p.n_global, p.aim).count;
+  float M = lane < nc ? m0 : -INFINITY;
+  for (int c = lane + 64; c < nc; c += 64) M = fmaxf(M, p.ws_m[s0 + c]);
+  M = wave_max_dpp(M);
   const float Mu = (M == -INFINITY) ? 0.f : M;
+  float os[NS][NV];
+#pragma unroll
+  for (int g = 0; g < NS; ++g)
+#pragma unroll
+    for (int i = 0; i < NV; ++i) os[g][i] = 0.f;
   float lsum = 0.f;
-  for (int c = lane; c < nc; c += 64) lsum = fmaf(exp2f(p.ws_m[s0 + c] - Mu), p.ws_l[s0 + c], lsum);
-  lsum = wave_sum(lsum);
-  float osum = 0.f;
-  if (grp < groups)
-    for (int c = grp; c < nc; c += groups) osum = fmaf(exp2f(p.ws_m[s0 + c] - Mu), p.ws_o[(s0 + c) * d + dd], osum);
-  part[threadIdx.x] = osum;
-  __syncthreads();
-  if (grp != 0) return;
-  for (int g = 1; g < groups; ++g) osum += part[g * d + dd];
-  const float out = lsum > 0.f ? osum / lsum : 0.f;
-  if (obf16) ((uint16_t*)o)[(int64_t)bh * d + dd] = (uint16_t)f32_to_bf16_rne(out);
-  else ((float*)o)[(int64_t)bh * d + dd] = out;
-  if (lse && dd == 0) lse[bh] = lsum > 0.f ? (M + __log2f(lsum)) * kLn2 : -INFINITY;
+  for (int cb = 0; cb < nc; cb += 64) {  // 64 chunks' weights, one a lane
+    const bool in = cb + lane < nc;
+    const float w = in ? __builtin_amdgcn_exp2f((cb == 0 ? m0 : p.ws_m[s0 + cb + lane]) - Mu) : 0.f;
+    lsum = in ? fmaf(w, cb == 0 ? l0 : p.ws_l[s0 + cb + lane], lsum) : lsum;
+    for (int c0 = cb; c0 < min(nc, cb + 64); c0 += kMergeQ4) {
+      float y[NS][NV];
+#pragma unroll
+      for (int g = 0; g < NS; ++g)
+#pragma unroll
+        for (int i = 0; i < NV; ++i) y[g][i] = x[g][i];
+      if (c0 + kMergeQ4 < nc) load_rows(c0 + kMergeQ4);
+#pragma unroll
+      for (int g = 0; g < NS; ++g) {
+        const int c = c0 + (WIDE ? wave : g);
+        const float wc = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(w), c - cb));
+#pragma unroll
+        for (int i = 0; i < NV; ++i) os[g][i] = c < nc ? fmaf(wc, y[g][i], os[g][i]) : os[g][i];
+      }
+    }
+  }
+  lsum = wave_sum_dpp(lsum);
+  if constexpr (WIDE) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) part[wave][lane + 64 * i] = os[0][i];
+    __syncthreads();
+    if (wave != 0) return;
+  }
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    float sum = os[0][i];
+#pragma unroll
+    for (int g = 1; g < kMergeQ4; ++g) sum += WIDE ? part[g][lane + 64 * i] : os[WIDE ? 0 : g][i];
+    const float out = lsum > 0.f ? sum / lsum : 0.f;
+    const int c = lane + 64 * i;
+    if (c < d) {
+      if (obf16) ((uint16_t*)o)[(int64_t)bh * d + c] = (uint16_t)f32_to_bf16_rne(out);
+      else ((float*)o)[(int64_t)bh * d + c] = out;
+    }
+  }
+  if (lse && lane == 0) lse[bh] = lsum > 0.f ? (M + __log2f(lsum)) * kLn2 : -INFINITY;
+}
+
+template <int NV>
+void launch_q4_combine(const DecParams& p, const DecodeArgs& a, hipStream_t stream) {
+  const int rows = a.B * a.Hq;
+  // one wavefront a row where a row's chunks are few or the rows fill the chip
+  if (p.nch <= 2 * kMergeQ4 || rows >= 8192)
+    hipLaunchKernelGGL((sfa_decode_q4_combine_kernel<NV, false>), dim3((rows + 3) / 4), dim3(256), 0, stream, p, rows, a.d,
+                       a.o, a.obf16, a.lse);
+  else
+    hipLaunchKernelGGL((sfa_decode_q4_combine_kernel<NV, true>), dim3(rows), dim3(64 * kMergeQ4), 0, stream, p, rows, a.d,
+                       a.o, a.obf16, a.lse);
 }
 
 template <int D, int GP, int KC8>
@@ -502,8 +588,9 @@ hipError_t launch_attn_decode_q4(const DecodeArgs& a, hipStream_t stream) {
   else launch_q4_g<256>(p, a, stream);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(sfa_decode_q4_combine_kernel, dim3(a.B * a.Hq), dim3(kMergeQ4), 0, stream, p, a.d,
-                     kMergeQ4 / a.d, a.o, a.obf16, a.lse);
+  if (a.d <= 64) launch_q4_combine<1>(p, a, stream);
+  else if (a.d <= 128) launch_q4_combine<2>(p, a, stream);
+  else launch_q4_combine<4>(p, a, stream);
   return hipGetLastError();
 }
 
