@@ -578,7 +578,8 @@ sfa_status sfa_rope_encode(const void* x, const int64_t* x_strides, const int32_
 /*
  * Backward of sfa_rope_encode with the straight-through estimator (Sec. 3.1,
  * Eq. (6): the gradient of a coordinate is that of its code value on the
- * support and 0 elsewhere):  dx = R(pos)^T scatter(idx, dval).
+ * support and 0 elsewhere):  dx = R(pos)^T scatter(idx, dval), the rotation in
+ * float32 (sines and cosines as sfa_rope's).
  * idx, dval [B, H, n, k] contiguous: the code's indices (idx_t) and the float32
  *           gradients of its values, as sfa_attn_bwd returns them.  Indices are
  *           distinct within a row; they are masked into range before use.

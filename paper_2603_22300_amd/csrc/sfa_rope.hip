@@ -129,8 +129,8 @@ __device__ __forceinline__ void unit_turns(const RopePlan& pl, const int32_t* po
   }
 }
 
-// The two runs of a unit, rotated in place.
-template <int VP>
+// The two runs of a unit, rotated in place (F32: in float32; else rounded once).
+template <int VP, bool F32 = false>
 __device__ __forceinline__ void unit_rotate(bool neighbours, const float (&c)[VP], const float (&s)[VP],
                                             float (&a)[VP], float (&b)[VP]) {
   float r[2 * VP];
@@ -138,8 +138,14 @@ __device__ __forceinline__ void unit_rotate(bool neighbours, const float (&c)[VP
   for (int i = 0; i < VP; ++i) { r[i] = a[i]; r[VP + i] = b[i]; }
 #pragma unroll
   for (int i = 0; i < VP; ++i) {
+    const float x1 = neighbours ? r[2 * i] : a[i], x2 = neighbours ? r[2 * i + 1] : b[i];
     float y1, y2;
-    rotate(neighbours ? r[2 * i] : a[i], neighbours ? r[2 * i + 1] : b[i], c[i], s[i], y1, y2);
+    if constexpr (F32) {
+      y1 = fmaf(x1, c[i], -(x2 * s[i]));
+      y2 = fmaf(x2, c[i], x1 * s[i]);
+    } else {
+      rotate(x1, x2, c[i], s[i], y1, y2);
+    }
     if (neighbours) { r[2 * i] = y1; r[2 * i + 1] = y2; }
     else { r[i] = y1; r[VP + i] = y2; }
   }
@@ -193,44 +199,62 @@ __global__ __launch_bounds__(256) void sfa_rope_encode_kernel(RopePlan pl, RopeA
   const int slices = (a.H + a.heads - 1) / a.heads;
   const int half = pl.rot / 2;
   constexpr int EP = SAME ? E / 2 : E;
-  int pair[EP], part[EP];
+  int axis[EP], part[EP];
   float sign[EP];
+  double freq[EP];
   bool turned[EP];
 #pragma unroll
   for (int e = 0; e < EP; ++e) {
     const int c = min(lane + 64 * e, a.d - 1);
     turned[e] = SAME || c < pl.rot;
     const bool second = pl.neighbours ? (c & 1) : c >= half;
-    pair[e] = turned[e] ? (pl.neighbours ? c >> 1 : (second ? c - half : c)) : 0;
+    const int pair = turned[e] ? (pl.neighbours ? c >> 1 : (second ? c - half : c)) : 0;
+    axis[e] = pl.axis[pair];
+    freq[e] = pl.freq[pair];
     part[e] = !turned[e] ? c : pl.neighbours ? c ^ 1 : (second ? c - half : c + half);
     sign[e] = second ? 1.f : -1.f;
   }
-  for (int64_t w = (int64_t)blockIdx.x * 4 + wave; w < ntok * slices; w += (int64_t)gridDim.x * 4) {
-    const int slice = (int)(w / ntok);
-    const int64_t tok = w - slice * ntok;
-    const int b = (int)(tok / a.n), t = (int)(tok - (int64_t)b * a.n);
-    const int h0 = slice * a.heads, h1 = min(a.H, h0 + a.heads);
-    float co[EP], si[EP];
+  const int64_t items = ntok * slices, stride = (int64_t)gridDim.x * 4;
+  int64_t w = (int64_t)blockIdx.x * 4 + wave;
+  if (w >= items) return;  // uniform per wave
+  // A row's words, and a token's positions, are loaded one row ahead, past the end
+  // of a token's heads too.
+  uint32_t nx[E], np[SAME ? 1 : E];
+  auto load_row = [&](int64_t o) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int c = min(lane + 64 * e, a.d - 1);
+      nx[e] = XB ? (uint32_t)((const uint16_t*)a.x + o)[c] : ((const uint32_t*)a.x + o)[c];
+      if constexpr (!SAME)
+        np[e] = XB ? (uint32_t)((const uint16_t*)a.x + o)[part[e]] : ((const uint32_t*)a.x + o)[part[e]];
+    }
+  };
+  int npos[EP];
+  int slice, b, t;
+  int64_t tok;
+  auto open_item = [&]() {
+    slice = (int)(w / ntok);
+    tok = w - slice * ntok;
+    b = (int)(tok / a.n);
+    t = (int)(tok - (int64_t)b * a.n);
     const int32_t* pos = a.pos + b * a.pos_batch + t;
 #pragma unroll
+    for (int e = 0; e < EP; ++e) npos[e] = pos[axis[e] * a.pos_axis];
+    load_row(b * a.xs[0] + t * a.xs[2] + slice * a.heads * a.xs[1]);
+  };
+  auto value = [](uint32_t v) { return XB ? bf16_bits_to_f32(v) : __uint_as_float(v); };
+  open_item();
+  while (true) {
+    const int h0 = slice * a.heads, h1 = min(a.H, h0 + a.heads);
+    const int64_t x0 = b * a.xs[0] + t * a.xs[2], o_base = ((int64_t)b * a.H * a.n + t) * a.k;
+    float co[EP], si[EP];
+#pragma unroll
     for (int e = 0; e < EP; ++e) {
-      turn((double)pos[pl.axis[pair[e]] * a.pos_axis] * pl.freq[pair[e]], co[e], si[e]);
+      turn((double)npos[e] * freq[e], co[e], si[e]);
       if (!SAME) si[e] *= sign[e];
     }
-    const int64_t xb = b * a.xs[0] + t * a.xs[2];
-    uint32_t nx[E], np[SAME ? 1 : E];
-    auto load_row = [&](int h) {
-      const int64_t o = xb + h * a.xs[1];
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const int c = min(lane + 64 * e, a.d - 1);
-        nx[e] = XB ? (uint32_t)((const uint16_t*)a.x + o)[c] : ((const uint32_t*)a.x + o)[c];
-        if constexpr (!SAME)
-          np[e] = XB ? (uint32_t)((const uint16_t*)a.x + o)[part[e]] : ((const uint32_t*)a.x + o)[part[e]];
-      }
-    };
-    auto value = [](uint32_t v) { return XB ? bf16_bits_to_f32(v) : __uint_as_float(v); };
-    load_row(h0);
+    w += stride;
+    const bool more = w < items;
     for (int h = h0; h < h1; ++h) {
       uint32_t bits[E], key[E];
       if constexpr (SAME) {
@@ -251,26 +275,30 @@ __global__ __launch_bounds__(256) void sfa_rope_encode_kernel(RopePlan pl, RopeA
       }
 #pragma unroll
       for (int e = 0; e < E; ++e) key[e] = topk_key(bits[e], lane + 64 * e < a.d);
-      if (h + 1 < h1) load_row(h + 1);
+      if (h + 1 < h1) load_row(x0 + (h + 1) * a.xs[1]);
+      else if (more) open_item();
       bool sel[E];
       topk_select<E>(key, a.k, sel);
       int slot[E];
       topk_slots<E>(sel, slot);
-      const int64_t o0 = (((int64_t)b * a.H + h) * a.n + t) * a.k;
+      const int64_t o0 = o_base + (int64_t)h * a.n * a.k;
 #pragma unroll
       for (int e = 0; e < E; ++e)
         if (sel[e] && slot[e] < a.k) store_code(a.idx, a.val, o0 + slot[e], lane + 64 * e, bits[e], ifmt, vfmt);
     }
+    if (!more) break;
   }
 }
 
-// dx = R^T scatter(idx, dval).  A wavefront takes 64 / U tokens (U: units of a
+// dx = R^T scatter(idx, dval).  A wavefront takes R = 64 / U tokens (U: units of a
 // row), a lane one unit of one of them, and the heads of its slice in turn: the
-// code entries are scattered into float32 rows of LDS, each lane reads its unit
-// back, turns and stores it, and the entries' places are cleared again.
-// Bound by memory: it writes d values for the k entries it reads.
-constexpr int kBwdLds = 4 * 512;  // floats; a wavefront's (64 / U) d are at most 512 (U >= d / 8), or d where U >= 64
-template <int VP, typename YT>
+// code entries, NE a lane and loaded a head ahead, are scattered into float32 rows
+// of LDS, each lane reads its unit back, turns and stores it, and the entries'
+// places are cleared again.  The rotation is float32 here (a product and an fma, off
+// by 2^-24 of each term: no selection hangs on it).  Bound by memory: it writes d
+// values for the k entries it reads.
+constexpr int kBwdLds = 4 * 512;  // floats; a wavefront's R d are at most 512 (U >= d / 8), or d where U >= 64
+template <int VP, int NE, typename YT>
 __global__ __launch_bounds__(256) void sfa_rope_bwd_kernel(RopePlan pl, RopeArgs a) {
   __shared__ float rows_lds[kBwdLds];
   const int lane = threadIdx.x & 63;
@@ -282,6 +310,30 @@ __global__ __launch_bounds__(256) void sfa_rope_bwd_kernel(RopePlan pl, RopeArgs
   const int64_t tok0 = ((int64_t)blockIdx.x * 4 + wave) * R;
   const int here = (int)min((int64_t)R, ntok - tok0);
   if (here <= 0) return;  // uniform per wave; no workgroup barrier below
+  const int h0 = blockIdx.y * a.heads, h1 = min(a.H, h0 + a.heads);
+
+  // Entry e of the wave's tokens: token e / k (exact: e < 2^11, so (e + 1/2) / k is
+  // 1/(2k) or more from an integer).  Lanes past the last entry repeat it.
+  const float inv_k = 1.f / (float)a.k;
+  int64_t at[NE];
+  int place[NE], ci[NE];
+  float cg[NE];
+#pragma unroll
+  for (int j = 0; j < NE; ++j) {
+    const int e = min(lane + 64 * j, here * a.k - 1), r = (int)(((float)e + 0.5f) * inv_k);
+    const int64_t tok = tok0 + r, b = a.B == 1 ? 0 : tok / a.n;
+    at[j] = ((b * a.H + h0) * a.n + (tok - b * a.n)) * a.k + (e - r * a.k);
+    place[j] = r * d;
+  }
+  auto load_entries = [&]() {
+#pragma unroll
+    for (int j = 0; j < NE; ++j) {
+      ci[j] = min(load_idx(a.idx, at[j], a.ifmt, 255), d - 1);
+      cg[j] = a.dval[at[j]];
+      at[j] += (int64_t)a.n * a.k;
+    }
+  };
+  load_entries();
   for (int i = lane; i < R * d; i += 64) rows[i] = 0.f;
 
   float c[NIT][VP], s[NIT][VP];
@@ -296,25 +348,18 @@ __global__ __launch_bounds__(256) void sfa_rope_bwd_kernel(RopePlan pl, RopeArgs
     act[it] = row[it] < here;
     const int64_t tok = tok0 + (act[it] ? row[it] : 0);
     const int64_t b = tok / a.n, t = tok - b * a.n;
-    turned[it] = un.turned; off0[it] = un.off0; off1[it] = un.off1; two[it] = un.n1 == VP;
+    off0[it] = un.off0; off1[it] = un.off1; two[it] = un.n1 == VP; turned[it] = un.turned;
     unit_turns<VP>(pl, a.pos + b * a.pos_batch + t, a.pos_axis, act[it] && un.turned, un.pair, c[it], s[it]);
-    yo[it] = b * a.ys[0] + t * a.ys[2];
+    yo[it] = b * a.ys[0] + t * a.ys[2] + h0 * a.ys[1];
   }
-  const int h0 = blockIdx.y * a.heads, h1 = min(a.H, h0 + a.heads);
-  const float inv_k = 1.f / (float)a.k;
   for (int h = h0; h < h1; ++h) {
-    // entry e of the wave's tokens: token e / k (exact: e < 2^11, so (e + 1/2)
-    // / k is 1/(2k) or more from an integer)
-    auto entry = [&](int e, int& r, int64_t& at) {
-      r = (int)(((float)e + 0.5f) * inv_k);
-      const int64_t tok = tok0 + r, b = a.B == 1 ? 0 : tok / a.n;
-      at = ((b * a.H + h) * a.n + (tok - b * a.n)) * a.k + (e - r * a.k);
-    };
-    for (int e = lane; e < here * a.k; e += 64) {
-      int r; int64_t at;
-      entry(e, r, at);
-      rows[r * d + min(load_idx(a.idx, at, a.ifmt, 255), d - 1)] = a.dval[at];
+    int here_at[NE];
+#pragma unroll
+    for (int j = 0; j < NE; ++j) {
+      here_at[j] = place[j] + ci[j];
+      rows[here_at[j]] = cg[j];
     }
+    if (h + 1 < h1) load_entries();
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
@@ -328,20 +373,16 @@ __global__ __launch_bounds__(256) void sfa_rope_bwd_kernel(RopePlan pl, RopeArgs
 #pragma unroll
         for (int i = 0; i < VP; ++i) q[i] = 0.f;
       }
-      if (turned[it]) unit_rotate<VP>(pl.neighbours, c[it], s[it], p, q);
-      YT* y = (YT*)a.y + yo[it] + h * a.ys[1];
+      if (turned[it]) unit_rotate<VP, true>(pl.neighbours, c[it], s[it], p, q);
+      YT* y = (YT*)a.y + yo[it];
       store_vec<VP>(y + off0[it], p);
       if (two[it]) store_vec<VP>(y + off1[it], q);
+      yo[it] += a.ys[1];
     }
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    for (int e = lane; e < here * a.k; e += 64) {
-      int r; int64_t at;
-      entry(e, r, at);
-      rows[r * d + min(load_idx(a.idx, at, a.ifmt, 255), d - 1)] = 0.f;
-    }
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+    for (int j = 0; j < NE; ++j) rows[here_at[j]] = 0.f;
   }
 }
 
@@ -395,6 +436,13 @@ void launch_encode_e(const RopePlan& pl, const RopeArgs& a, dim3 grid, hipStream
   else launch_encode_s<4, XB>(pl, a, grid, stream);
 }
 
+template <int VP, int NE>
+void launch_bwd_t(const RopePlan& pl, const RopeArgs& a, dim3 grid, hipStream_t stream) {
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, pl, a); };
+  if (a.ybf16) go(sfa_rope_bwd_kernel<VP, NE, uint16_t>);
+  else go(sfa_rope_bwd_kernel<VP, NE, float>);
+}
+
 }  // namespace
 
 hipError_t launch_rope(const RopePlan& pl, RopeArgs a, hipStream_t stream) {
@@ -427,9 +475,16 @@ hipError_t launch_rope_encode_bwd(const RopePlan& pl, RopeArgs a, hipStream_t st
   const int64_t blocks = ((int64_t)a.B * a.n + 4 * a.tokens - 1) / (4 * a.tokens);
   a.heads = heads_per_slice(blocks, a.H, 2048);
   const dim3 grid((unsigned)blocks, (unsigned)((a.H + a.heads - 1) / a.heads));
-  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, pl, a); };
-  if (vec) a.ybf16 ? go(sfa_rope_bwd_kernel<4, uint16_t>) : go(sfa_rope_bwd_kernel<4, float>);
-  else a.ybf16 ? go(sfa_rope_bwd_kernel<1, uint16_t>) : go(sfa_rope_bwd_kernel<1, float>);
+  // code entries a lane holds: at most 64 k / U, k <= 8 U (VP = 4) or 2 U
+  const int ne = (a.tokens * a.k + 63) / 64;
+  if (vec) {
+    if (ne <= 1) launch_bwd_t<4, 1>(pl, a, grid, stream);
+    else if (ne <= 2) launch_bwd_t<4, 2>(pl, a, grid, stream);
+    else if (ne <= 4) launch_bwd_t<4, 4>(pl, a, grid, stream);
+    else launch_bwd_t<4, 8>(pl, a, grid, stream);
+  } else {
+    launch_bwd_t<1, 4>(pl, a, grid, stream);
+  }
   return hipGetLastError();
 }
 

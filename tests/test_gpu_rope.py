@@ -17,12 +17,15 @@ pytestmark = pytest.mark.gpu
 DEV = "cuda"
 
 
-def _bound(x, y, rot, pairing, bf16):
+def _bound(x, y, rot, pairing, bf16, f32=False):
     u, v = oracle.rope_pairs(rot, pairing)
     mag = np.zeros_like(y)
     m = np.abs(x[..., u]) + np.abs(x[..., v])
     mag[..., u], mag[..., v] = m, m
-    return ((2.0 ** -25 * mag + 2.0 ** -24 * np.abs(y)) * (1 + 2.0 ** -15) + 2.0 ** -8 * np.abs(y) * bf16 + 1e-45)
+    # f32: one of the two products is itself rounded to float32 (half a step, 2^-24 of at
+    # most |x1| or |x2|, as |sin| and |cos| are at most 1), the other enters an fma exactly
+    w = 2.0 ** -25 + f32 * 2.0 ** -24
+    return ((w * mag + 2.0 ** -24 * np.abs(y)) * (1 + 2.0 ** -15) + 2.0 ** -8 * np.abs(y) * bf16 + 1e-45)
 
 
 def _positions(A, B, n, seed, far):
@@ -160,7 +163,7 @@ def test_rope_encode_bwd(case, k, bf16):
     np.put_along_axis(dense, idx.long().cpu().numpy(), g.double().cpu().numpy(), -1)
     want = oracle.rope(dense, pos, axis, freq, pairing, inverse=True)
     got = dx.double().cpu().numpy()
-    bound = _bound(dense, want, plan.rot, pairing, bf16)
+    bound = _bound(dense, want, plan.rot, pairing, bf16, f32=True)
     assert (np.abs(got - want) <= bound).all()
     assert torch.equal(sfa.sfa_rope_encode_bwd(idx, g, pt, plan, dx_dtype=packed.dtype), dx)
     rng = np.random.default_rng(k)
