@@ -160,9 +160,9 @@ __device__ __forceinline__ void unit_rotate(bool neighbours, const float (&c)[VP
 template <int VP, typename XT, typename YT>
 __global__ __launch_bounds__(256) void sfa_rope_kernel(RopePlan pl, RopeArgs a) {
   const int U = a.units, r = threadIdx.x / U, u = threadIdx.x - r * U;
-  const int64_t tok = (int64_t)blockIdx.x * (256 / U) + r;
-  if (r >= 256 / U || tok >= (int64_t)a.B * a.n) return;
-  const int b = (int)(tok / a.n), t = (int)(tok - (int64_t)b * a.n);
+  const uint32_t tok = blockIdx.x * (uint32_t)(256 / U) + r;  // (B * n < 2^31)
+  if (r >= 256 / U || tok >= (uint32_t)(a.B * a.n)) return;
+  const uint32_t b = a.B == 1 ? 0 : tok / (uint32_t)a.n, t = tok - b * a.n;
   const Unit<VP> un(pl, u);
   float c[VP], s[VP];
   unit_turns<VP>(pl, a.pos + b * a.pos_batch + t, a.pos_axis, un.turned, un.pair, c, s);
@@ -195,8 +195,7 @@ __global__ __launch_bounds__(256) void sfa_rope_encode_kernel(RopePlan pl, RopeA
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int ifmt = IF >= 0 ? IF : a.ifmt, vfmt = VF >= 0 ? VF : a.vfmt;
-  const int64_t ntok = (int64_t)a.B * a.n;
-  const int slices = (a.H + a.heads - 1) / a.heads;
+  const uint32_t ntok = (uint32_t)(a.B * a.n);  // (< 2^31)
   const int half = pl.rot / 2;
   constexpr int EP = SAME ? E / 2 : E;
   int axis[EP], part[EP];
@@ -214,9 +213,10 @@ __global__ __launch_bounds__(256) void sfa_rope_encode_kernel(RopePlan pl, RopeA
     part[e] = !turned[e] ? c : pl.neighbours ? c ^ 1 : (second ? c - half : c + half);
     sign[e] = second ? 1.f : -1.f;
   }
-  const int64_t items = ntok * slices, stride = (int64_t)gridDim.x * 4;
-  int64_t w = (int64_t)blockIdx.x * 4 + wave;
-  if (w >= items) return;  // uniform per wave
+  const uint32_t stride = gridDim.x * 4;
+  uint32_t tok = blockIdx.x * 4 + wave;
+  if (tok >= ntok) return;  // uniform per wave
+  const int h0 = blockIdx.y * a.heads, h1 = min(a.H, h0 + a.heads);
   // A row's words, and a token's positions, are loaded one row ahead, past the end
   // of a token's heads too.
   uint32_t nx[E], np[SAME ? 1 : E];
@@ -230,22 +230,18 @@ __global__ __launch_bounds__(256) void sfa_rope_encode_kernel(RopePlan pl, RopeA
     }
   };
   int npos[EP];
-  int slice, b, t;
-  int64_t tok;
-  auto open_item = [&]() {
-    slice = (int)(w / ntok);
-    tok = w - slice * ntok;
-    b = (int)(tok / a.n);
-    t = (int)(tok - (int64_t)b * a.n);
+  uint32_t b, t;
+  auto open_token = [&]() {
+    b = a.B == 1 ? 0 : tok / (uint32_t)a.n;
+    t = tok - b * a.n;
     const int32_t* pos = a.pos + b * a.pos_batch + t;
 #pragma unroll
     for (int e = 0; e < EP; ++e) npos[e] = pos[axis[e] * a.pos_axis];
-    load_row(b * a.xs[0] + t * a.xs[2] + slice * a.heads * a.xs[1]);
+    load_row(b * a.xs[0] + t * a.xs[2] + h0 * a.xs[1]);
   };
   auto value = [](uint32_t v) { return XB ? bf16_bits_to_f32(v) : __uint_as_float(v); };
-  open_item();
+  open_token();
   while (true) {
-    const int h0 = slice * a.heads, h1 = min(a.H, h0 + a.heads);
     const int64_t x0 = b * a.xs[0] + t * a.xs[2], o_base = ((int64_t)b * a.H * a.n + t) * a.k;
     float co[EP], si[EP];
 #pragma unroll
@@ -253,8 +249,8 @@ __global__ __launch_bounds__(256) void sfa_rope_encode_kernel(RopePlan pl, RopeA
       turn((double)npos[e] * freq[e], co[e], si[e]);
       if (!SAME) si[e] *= sign[e];
     }
-    w += stride;
-    const bool more = w < items;
+    tok += stride;  // (no wrap: ntok and the grid's wavefronts are below 2^31)
+    const bool more = tok < ntok;
     for (int h = h0; h < h1; ++h) {
       uint32_t bits[E], key[E];
       if constexpr (SAME) {
@@ -276,7 +272,7 @@ __global__ __launch_bounds__(256) void sfa_rope_encode_kernel(RopePlan pl, RopeA
 #pragma unroll
       for (int e = 0; e < E; ++e) key[e] = topk_key(bits[e], lane + 64 * e < a.d);
       if (h + 1 < h1) load_row(x0 + (h + 1) * a.xs[1]);
-      else if (more) open_item();
+      else if (more) open_token();
       bool sel[E];
       topk_select<E>(key, a.k, sel);
       int slot[E];
@@ -306,10 +302,9 @@ __global__ __launch_bounds__(256) void sfa_rope_bwd_kernel(RopePlan pl, RopeArgs
   float* rows = rows_lds + wave * (kBwdLds / 4);
   const int U = a.units, R = a.tokens, d = a.d;
   constexpr int NIT = VP == 1 ? 2 : 1;  // up to 128 units where VP = 1
-  const int64_t ntok = (int64_t)a.B * a.n;
-  const int64_t tok0 = ((int64_t)blockIdx.x * 4 + wave) * R;
-  const int here = (int)min((int64_t)R, ntok - tok0);
-  if (here <= 0) return;  // uniform per wave; no workgroup barrier below
+  const uint32_t ntok = (uint32_t)(a.B * a.n), tok0 = (blockIdx.x * 4 + wave) * (uint32_t)R;  // (< 2^31)
+  if (tok0 >= ntok) return;  // uniform per wave; no workgroup barrier below
+  const int here = (int)min((uint32_t)R, ntok - tok0);
   const int h0 = blockIdx.y * a.heads, h1 = min(a.H, h0 + a.heads);
 
   // Entry e of the wave's tokens: token e / k (exact: e < 2^11, so (e + 1/2) / k is
@@ -321,8 +316,8 @@ __global__ __launch_bounds__(256) void sfa_rope_bwd_kernel(RopePlan pl, RopeArgs
 #pragma unroll
   for (int j = 0; j < NE; ++j) {
     const int e = min(lane + 64 * j, here * a.k - 1), r = (int)(((float)e + 0.5f) * inv_k);
-    const int64_t tok = tok0 + r, b = a.B == 1 ? 0 : tok / a.n;
-    at[j] = ((b * a.H + h0) * a.n + (tok - b * a.n)) * a.k + (e - r * a.k);
+    const uint32_t tok = tok0 + r, b = a.B == 1 ? 0 : tok / (uint32_t)a.n;
+    at[j] = (((int64_t)b * a.H + h0) * a.n + (tok - b * a.n)) * a.k + (e - r * a.k);
     place[j] = r * d;
   }
   auto load_entries = [&]() {
@@ -346,8 +341,8 @@ __global__ __launch_bounds__(256) void sfa_rope_bwd_kernel(RopePlan pl, RopeArgs
     row[it] = v / U;
     const Unit<VP> un(pl, v - row[it] * U);
     act[it] = row[it] < here;
-    const int64_t tok = tok0 + (act[it] ? row[it] : 0);
-    const int64_t b = tok / a.n, t = tok - b * a.n;
+    const uint32_t tok = tok0 + (act[it] ? row[it] : 0);
+    const uint32_t b = a.B == 1 ? 0 : tok / (uint32_t)a.n, t = tok - b * a.n;
     off0[it] = un.off0; off1[it] = un.off1; two[it] = un.n1 == VP; turned[it] = un.turned;
     unit_turns<VP>(pl, a.pos + b * a.pos_batch + t, a.pos_axis, act[it] && un.turned, un.pair, c[it], s[it]);
     yo[it] = b * a.ys[0] + t * a.ys[2] + h0 * a.ys[1];
@@ -458,11 +453,16 @@ hipError_t launch_rope(const RopePlan& pl, RopeArgs a, hipStream_t stream) {
 }
 
 hipError_t launch_rope_encode(const RopePlan& pl, RopeArgs a, hipStream_t stream) {
-  // persistent waves: up to 32 per compute unit, 4 per workgroup
+  // A wavefront takes the heads of one token, about 32 rows (several tokens where
+  // the heads are fewer), and leaves the rest to the dispatcher: in a grid that just
+  // fills the chip, wavefronts of equal shares end far apart (32 heads x 32,768
+  // tokens: 275 us with 8192 wavefronts of four tokens, 221 with 32,768 of one).
   const int64_t ntok = (int64_t)a.B * a.n;
   a.heads = heads_per_slice(ntok, a.H, 4 * 2048);
-  const int64_t need = (ntok * ((a.H + a.heads - 1) / a.heads) + 3) / 4;
-  const dim3 grid((unsigned)(need < 2048 ? need : 2048));
+  const int64_t slices = (a.H + a.heads - 1) / a.heads, need = (ntok + 3) / 4;
+  const int64_t per = a.heads >= 32 ? 1 : 32 / a.heads, full = (2047 + slices) / slices;
+  const int64_t filled = need < full ? need : full, blocks = (need + per - 1) / per;
+  const dim3 grid((unsigned)(blocks > filled ? blocks : filled), (unsigned)slices);
   if (a.xbf16) launch_encode_e<true>(pl, a, grid, stream);
   else launch_encode_e<false>(pl, a, grid, stream);
   return hipGetLastError();
