@@ -2,10 +2,15 @@
 // (Sec. 3.1, Eqs. (3)-(4)), quantisation of code values and value rows to signed
 // 4-bit numbers, q = round-half-even(x / s) in [-7, 7], and the cache write.
 //
-// One wavefront per (token, KV head) row.  Lane l holds key coordinates l + 64 e
-// for the selection (sfa_topk.h) and value coordinates 2 l + 128 i, 2 l + 1 + 128 i:
-// the 32 coordinates of one scale are then one 16-lane row, whose maximum is four
-// DPP steps, and a lane's two numbers are a byte.
+// One wavefront per (token, KV head) row, heads of a token side by side (packed
+// buffers are read in order), the next row's words and slot in flight while the
+// current one is coded.  Lane l holds key coordinates l + 64 e for the selection
+// (sfa_topk.h) and value coordinates 2 l + 128 i, 2 l + 1 + 128 i: the 32
+// coordinates of one scale are then one 16-lane row, whose maximum is four DPP
+// steps, and a lane's two numbers are a byte.  Bound by the selection, as the other
+// appends, so the row walk has no division and a number costs a product with the
+// scale's reciprocal: only where that lands next to a half is the correctly rounded
+// quotient, which decides, computed.
 #include "sfa_device.h"
 #include "sfa_launch.h"
 #include "sfa_topk.h"
@@ -21,14 +26,34 @@ __device__ __forceinline__ uint32_t row16_umax(uint32_t x) {
   return max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x140, 0xf, 0xf, false));  // row_mirror
 }
 
-__device__ __forceinline__ float quant4(float x, float s) {
-  return s > 0.f ? fminf(fmaxf(rintf(x / s), -7.f), 7.f) : 0.f;
+// N numbers of a row with scale s (uniform or not): round-half-even of the float32
+// quotient.  x * rcp(s) is off by less than 4 ulp, 2^-18 for the quotients here (at most
+// 7.1), so it rounds as the quotient does unless it lies within 2^-16 of a half; where
+// that happens, or the reciprocal leaves the normal range, the wavefront divides.
+template <int N>
+__device__ __forceinline__ void quant4(const float (&x)[N], float s, float (&q)[N]) {
+  const float r = __builtin_amdgcn_rcpf(s);
+  bool near = s < 0x1p-100f;
+  float y[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    y[i] = x[i] * r;
+    q[i] = rintf(y[i]);
+    near |= fabsf(fabsf(y[i] - q[i]) - 0.5f) < 0x1p-16f;
+  }
+  if (wave_ballot(near)) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) q[i] = s > 0.f ? rintf(x[i] / s) : 0.f;
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) q[i] = fminf(fmaxf(q[i], -7.f), 7.f);
 }
 
 __device__ __forceinline__ int64_t clamp_len(int64_t L, int64_t cap) { return L < 0 ? 0 : (L > cap ? cap : L); }
 
-// E: key coordinates per lane (d <= 64 E); KB, VB: bfloat16 keys / values in.
-template <int E, bool KB, bool VB>
+// E: key coordinates per lane (d <= 64 E); KB, VB: bfloat16 keys / values in; V2: a
+// lane's two values start on a boundary of two, and are one load.
+template <int E, bool KB, bool VB, bool V2>
 __global__ __launch_bounds__(256) void sfa_kv_append_q4_kernel(AppendQ4Args a) {
   constexpr int NV = E <= 2 ? 1 : 2;  // value pairs per lane
   __shared__ uint16_t ent_lds[4][256];
@@ -36,110 +61,177 @@ __global__ __launch_bounds__(256) void sfa_kv_append_q4_kernel(AppendQ4Args a) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   uint16_t* ent = ent_lds[wave];
   const int64_t cap = a.table ? (int64_t)a.max_pages * a.page_size : a.page_size;
-  const int64_t rows = (int64_t)a.B * a.T * a.Hkv;
   const int groups = a.d / 32;
-  for (int64_t w = (int64_t)blockIdx.x * 4 + wave; w < rows; w += (int64_t)gridDim.x * 4) {
-    const int64_t tok = w / a.Hkv;  // heads of a token side by side: packed buffers are read in order
-    const int h = (int)(w - tok * a.Hkv);
-    const int64_t b = tok / a.T, t = tok - b * a.T;
-    // the cache row (uniform per wave)
-    int64_t page, slot;
+
+  // (b, t, h) of the wave's row, stepped by the grid's wavefronts
+  const int64_t w = (int64_t)blockIdx.x * 4 + wave;
+  if (w >= (int64_t)a.B * a.T * a.Hkv) return;  // uniform per wave
+  int h = (int)(w % a.Hkv);
+  int64_t t = w / a.Hkv;
+  int b = (int)(t / a.T);
+  t -= (int64_t)b * a.T;
+
+  uint32_t nk[E], nv[NV][2];
+  int64_t nrow;  // cache row, or -1: not written
+  int64_t norow;
+  auto load_row = [&]() {
+    const int64_t ko = b * a.st[0] + h * a.st[1] + t * a.st[2], vo = b * a.st[3] + h * a.st[4] + t * a.st[5];
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int c = min(lane + 64 * e, a.d - 1);
+      nk[e] = KB ? (uint32_t)((const uint16_t*)a.k_new + ko)[c] : ((const uint32_t*)a.k_new + ko)[c];
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = min(2 * lane + 128 * i, a.d - 2);
+      if constexpr (VB && V2) {
+        const uint32_t two = *(const uint32_t*)((const uint16_t*)a.v_new + vo + c);
+        nv[i][0] = two << 16;
+        nv[i][1] = two & 0xffff0000u;
+      } else if constexpr (VB) {
+        nv[i][0] = (uint32_t)((const uint16_t*)a.v_new + vo)[c] << 16;
+        nv[i][1] = (uint32_t)((const uint16_t*)a.v_new + vo)[c + 1] << 16;
+      } else if constexpr (V2) {
+        const uint2 two = *(const uint2*)((const uint32_t*)a.v_new + vo + c);
+        nv[i][0] = two.x;
+        nv[i][1] = two.y;
+      } else {
+        nv[i][0] = ((const uint32_t*)a.v_new + vo)[c];
+        nv[i][1] = ((const uint32_t*)a.v_new + vo)[c + 1];
+      }
+    }
+    int64_t page = -1, slot = 0;
     if (a.slots) {
-      const int64_t s = a.slots[b * a.T + t];
-      if (s < 0 || s >= (int64_t)a.num_pages * a.page_size) continue;
-      page = s / a.page_size;
-      slot = s - page * a.page_size;
+      const int s = __builtin_amdgcn_readfirstlane(a.slots[(int64_t)b * a.T + t]);
+      if (s >= 0 && s < a.num_pages * a.page_size) {  // (below 2^31)
+        page = a.log2P >= 0 ? s >> a.log2P : (uint32_t)s / (uint32_t)a.page_size;
+        slot = s - page * a.page_size;
+      }
     } else {
       const int c = a.n_new ? a.n_new[b] : a.T;
       const int64_t pos = clamp_len(a.seq_len[b], cap) + t;
-      if (t >= c || pos >= cap) continue;
-      page = b;
-      slot = pos;
-      if (a.table) {
-        page = a.table[b * a.max_pages + pos / a.page_size];
-        slot = pos % a.page_size;
-        if (page < 0 || page >= a.num_pages) continue;
+      if (t < c && pos < cap) {
+        page = b;
+        slot = pos;
+        if (a.table) {
+          page = a.table[(int64_t)b * a.max_pages + (pos >> a.log2P)];
+          slot = pos & (a.page_size - 1);
+          if (page >= a.num_pages) page = -1;
+        }
       }
     }
-    const int64_t crow = (page * a.Hkv + h) * a.page_size + slot;
-    const int64_t ko = b * a.st[0] + h * a.st[1] + t * a.st[2], vo = b * a.st[3] + h * a.st[4] + t * a.st[5];
-
-    // codes
+    nrow = page < 0 ? -1 : (page * a.Hkv + h) * a.page_size + slot;
+    norow = ((int64_t)b * a.Hkv + h) * a.T + t;
+  };
+  load_row();
+  while (true) {
+    const int64_t crow = nrow, orow = norow;
     uint32_t bits[E], key[E], km = 0;
+    float x[NV][2];
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-      const int c = lane + 64 * e, cc = min(c, a.d - 1);
-      bits[e] = KB ? (uint32_t)((const uint16_t*)a.k_new + ko)[cc] << 16 : ((const uint32_t*)a.k_new + ko)[cc];
-      key[e] = topk_key(bits[e], c < a.d);
+      bits[e] = KB ? nk[e] << 16 : nk[e];
+      key[e] = topk_key(bits[e], lane + 64 * e < a.d);
       km = max(km, key[e]);
     }
-    bool sel[E];
-    topk_select<E>(key, a.k, sel);
-    int sl[E];
-    topk_slots<E>(sel, sl);
-    // the kept values' largest magnitude is the row's: the largest key, |bits| + 1
-    const float ks = __uint_as_float(wave_umax(km) - 1u) / 7.f;
-#pragma unroll
-    for (int e = 0; e < E; ++e)
-      if (sel[e] && sl[e] < a.k)
-        ent[sl[e]] = (uint16_t)((lane + 64 * e) | ((int)quant4(__uint_as_float(bits[e]), ks) & 15) << 8);
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    for (int i = lane; i < a.k / 2; i += 64) {
-      const uint32_t two = ((const uint32_t*)ent)[i];
-      ((uint16_t*)(a.kc_idx + crow * a.k))[i] = (uint16_t)((two & 255u) | ((two >> 8) & 0xff00u));
-      (a.kc_val + crow * (a.k / 2))[i] = (uint8_t)(((two >> 8) & 15u) | ((two >> 20) & 0xf0u));
-    }
-    if (lane == 0) a.kc_scale[crow] = ks;
-    const int64_t orow = (b * a.Hkv + h) * a.T + t;
-    if (a.k_idx)
-      for (int i = lane; i < a.k; i += 64) {
-        const int v = ent[i];
-        a.k_idx[orow * a.k + i] = (int16_t)(v & 255);
-        a.k_val[orow * a.k + i] = (float)((int)((uint32_t)v << 20) >> 28) * ks;
-      }
-    __builtin_amdgcn_wave_barrier();
-
-    // values
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int c = 2 * lane + 128 * i;
-      const bool in = c < a.d;
-      float x0 = 0.f, x1 = 0.f;
-      if (in) {
-        x0 = VB ? bf16_bits_to_f32(((const uint16_t*)a.v_new + vo)[c]) : ((const float*)a.v_new + vo)[c];
-        x1 = VB ? bf16_bits_to_f32(((const uint16_t*)a.v_new + vo)[c + 1]) : ((const float*)a.v_new + vo)[c + 1];
+      const bool in = 2 * lane + 128 * i < a.d;
+      x[i][0] = in ? __uint_as_float(nv[i][0]) : 0.f;
+      x[i][1] = in ? __uint_as_float(nv[i][1]) : 0.f;
+    }
+    h += a.step_h;
+    t += a.step_t;
+    b += a.step_b;
+    if (h >= a.Hkv) { h -= a.Hkv; ++t; }
+    if (t >= a.T) { t -= a.T; ++b; }
+    const bool more = b < a.B;
+    if (more) load_row();
+    if (crow >= 0) {  // uniform per wave
+      bool sel[E];
+      topk_select<E>(key, a.k, sel);
+      int sl[E];
+      topk_slots<E>(sel, sl);
+      // the kept values' largest magnitude is the row's: the largest key, |bits| + 1
+      const float ks = __uint_as_float(wave_umax(km) - 1u) / 7.f;
+      float kx[E], q[E];
+#pragma unroll
+      for (int e = 0; e < E; ++e) kx[e] = sel[e] ? __uint_as_float(bits[e]) : 0.f;
+      quant4<E>(kx, ks, q);
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        if (sel[e] && sl[e] < a.k) ent[sl[e]] = (uint16_t)((lane + 64 * e) | ((int)q[e] & 15) << 8);
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      for (int i = lane; i < a.k / 2; i += 64) {
+        const uint32_t two = ((const uint32_t*)ent)[i];
+        ((uint16_t*)(a.kc_idx + crow * a.k))[i] = (uint16_t)((two & 255u) | ((two >> 8) & 0xff00u));
+        (a.kc_val + crow * (a.k / 2))[i] = (uint8_t)(((two >> 8) & 15u) | ((two >> 20) & 0xf0u));
       }
-      const uint32_t m = row16_umax(max(__float_as_uint(x0) & 0x7fffffffu, __float_as_uint(x1) & 0x7fffffffu));
-      const uint32_t sb = f32_to_bf16_rne(__uint_as_float(m) / 7.f);
-      const float s = bf16_bits_to_f32(sb);
-      const float q0 = quant4(x0, s), q1 = quant4(x1, s);
-      if (in) {
-        (a.v_cache + crow * (a.d / 2))[c / 2] = (uint8_t)(((int)q0 & 15) | ((int)q1 & 15) << 4);
-        if ((lane & 15) == 0) a.v_scale[crow * groups + c / 32] = (uint16_t)sb;
-        if (a.v_out)
-          *(uint32_t*)(a.v_out + orow * a.d + c) = f32_to_bf16_rne(q0 * s) | f32_to_bf16_rne(q1 * s) << 16;
+      if (lane == 0) a.kc_scale[crow] = ks;
+      if (a.k_idx)
+        for (int i = lane; i < a.k; i += 64) {
+          const int v = ent[i];
+          a.k_idx[orow * a.k + i] = (int16_t)(v & 255);
+          a.k_val[orow * a.k + i] = (float)((int)((uint32_t)v << 20) >> 28) * ks;
+        }
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const int c = 2 * lane + 128 * i;
+        const uint32_t m = row16_umax(max(__float_as_uint(x[i][0]) & 0x7fffffffu, __float_as_uint(x[i][1]) & 0x7fffffffu));
+        const uint32_t sb = f32_to_bf16_rne(__uint_as_float(m) / 7.f);
+        const float s = bf16_bits_to_f32(sb);
+        float vq[2];
+        quant4<2>(x[i], s, vq);
+        if (c < a.d) {
+          (a.v_cache + crow * (a.d / 2))[c / 2] = (uint8_t)(((int)vq[0] & 15) | ((int)vq[1] & 15) << 4);
+          if ((lane & 15) == 0) a.v_scale[crow * groups + c / 32] = (uint16_t)sb;
+          if (a.v_out)
+            *(uint32_t*)(a.v_out + orow * a.d + c) = f32_to_bf16_rne(vq[0] * s) | f32_to_bf16_rne(vq[1] * s) << 16;
+        }
       }
     }
+    if (!more) break;
   }
 }
 
-template <bool KB, bool VB>
-void launch_q4_t(const AppendQ4Args& a, dim3 grid, hipStream_t stream) {
+template <int E, bool KB, bool VB>
+void launch_q4_v(const AppendQ4Args& a, bool v2, dim3 grid, hipStream_t stream) {
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, a); };
-  if (a.d <= 64) go(sfa_kv_append_q4_kernel<1, KB, VB>);
-  else if (a.d <= 128) go(sfa_kv_append_q4_kernel<2, KB, VB>);
-  else go(sfa_kv_append_q4_kernel<4, KB, VB>);
+  if (v2) go(sfa_kv_append_q4_kernel<E, KB, VB, true>);
+  else go(sfa_kv_append_q4_kernel<E, KB, VB, false>);
+}
+
+template <bool KB, bool VB>
+void launch_q4_t(const AppendQ4Args& a, bool v2, dim3 grid, hipStream_t stream) {
+  if (a.d <= 64) launch_q4_v<1, KB, VB>(a, v2, grid, stream);
+  else if (a.d <= 128) launch_q4_v<2, KB, VB>(a, v2, grid, stream);
+  else launch_q4_v<4, KB, VB>(a, v2, grid, stream);
 }
 
 }  // namespace
 
-hipError_t launch_kv_append_q4(const AppendQ4Args& a, hipStream_t stream) {
-  const int64_t need = ((int64_t)a.B * a.T * a.Hkv + 3) / 4;
+hipError_t launch_kv_append_q4(AppendQ4Args a, hipStream_t stream) {
+  const int64_t rows = (int64_t)a.B * a.T * a.Hkv, need = (rows + 3) / 4;
   if (need > 0) {
-    const dim3 grid((unsigned)(need < 2048 ? need : 2048));
-    if (a.kbf16) a.vbf16 ? launch_q4_t<true, true>(a, grid, stream) : launch_q4_t<true, false>(a, grid, stream);
-    else a.vbf16 ? launch_q4_t<false, true>(a, grid, stream) : launch_q4_t<false, false>(a, grid, stream);
+    // eight rows a wavefront where they fill the chip eight times over, the rest left to
+    // the dispatcher (see launch_rope_encode)
+    const int64_t filled = need < 2048 ? need : 2048, blocks = (need + 7) / 8 > filled ? (need + 7) / 8 : filled;
+    const dim3 grid((unsigned)blocks);
+    a.log2P = -1;
+    if ((a.page_size & (a.page_size - 1)) == 0)
+      for (a.log2P = 0; (1 << a.log2P) < a.page_size;) ++a.log2P;
+    // the step of a wavefront's walk, in heads, tokens and sequences
+    int64_t step = 4 * blocks;
+    a.step_h = (int)(step % a.Hkv);
+    step /= a.Hkv;
+    a.step_t = (int)(step % a.T);
+    a.step_b = (int)(step / a.T);
+    const bool v2 = ((a.st[3] | a.st[4] | a.st[5]) & 1) == 0 && (uintptr_t)a.v_new % (a.vbf16 ? 4 : 8) == 0;
+    if (a.kbf16) a.vbf16 ? launch_q4_t<true, true>(a, v2, grid, stream) : launch_q4_t<true, false>(a, v2, grid, stream);
+    else a.vbf16 ? launch_q4_t<false, true>(a, v2, grid, stream) : launch_q4_t<false, false>(a, v2, grid, stream);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }

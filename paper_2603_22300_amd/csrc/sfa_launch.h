@@ -216,8 +216,9 @@ struct AppendQ4Args {
   int16_t* k_idx;
   float* k_val;
   uint16_t* v_out;
+  int log2P, step_h, step_t, step_b;  // set by the launcher
 };
-hipError_t launch_kv_append_q4(const AppendQ4Args& a, hipStream_t stream);
+hipError_t launch_kv_append_q4(AppendQ4Args a, hipStream_t stream);
 // seq_len[b] += the appended count, clamped to the capacity (sfa_cache.hip)
 hipError_t launch_kv_advance(int32_t* seq_len, const int32_t* n_new, int B, int T, int64_t cap,
                              hipStream_t stream);
