@@ -49,6 +49,15 @@ __device__ __forceinline__ void quant4(const float (&x)[N], float s, float (&q)[
   for (int i = 0; i < N; ++i) q[i] = fminf(fmaxf(q[i], -7.f), 7.f);
 }
 
+// x / 7, correctly rounded: the product with the rounded reciprocal and one fma
+// correction of its remainder (Markstein's theorem; checked over all significands),
+// the division itself where the remainder could leave the normal range.
+__device__ __forceinline__ float seventh(float x) {
+  const float r = 1.f / 7.f, q = x * r;
+  const float y = fmaf(fmaf(-7.f, q, x), r, q);
+  return wave_ballot(!(x >= 0x1p-90f && x < 0x1p126f)) ? x / 7.f : y;
+}
+
 __device__ __forceinline__ int64_t clamp_len(int64_t L, int64_t cap) { return L < 0 ? 0 : (L > cap ? cap : L); }
 
 // E: key coordinates per lane (d <= 64 E); KB, VB: bfloat16 keys / values in; V2: a
@@ -61,21 +70,23 @@ __global__ __launch_bounds__(256) void sfa_kv_append_q4_kernel(AppendQ4Args a) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   uint16_t* ent = ent_lds[wave];
   const int64_t cap = a.table ? (int64_t)a.max_pages * a.page_size : a.page_size;
-  const int groups = a.d / 32;
 
   // (b, t, h) of the wave's row, stepped by the grid's wavefronts
   const int64_t w = (int64_t)blockIdx.x * 4 + wave;
   if (w >= (int64_t)a.B * a.T * a.Hkv) return;  // uniform per wave
   int h = (int)(w % a.Hkv);
-  int64_t t = w / a.Hkv;
-  int b = (int)(t / a.T);
-  t -= (int64_t)b * a.T;
+  int t = (int)(w / a.Hkv % a.T);
+  int b = (int)(w / a.Hkv / a.T);
 
   uint32_t nk[E], nv[NV][2];
-  int64_t nrow;  // cache row, or -1: not written
-  int64_t norow;
+  // The row's place: its slot, or its position and page, as they are loaded (nothing
+  // waits for them before the row's turn).
+  int nplace = 0;
+  int64_t npos = 0, norow, len = 0;
+  int count = a.T, len_of = -1;  // of sequence len_of
+  int64_t ko = b * a.st[0] + h * a.st[1] + t * a.st[2], vo = b * a.st[3] + h * a.st[4] + t * a.st[5];
+  int64_t tok = (int64_t)b * a.T + t, out_row = ((int64_t)b * a.Hkv + h) * a.T + t;
   auto load_row = [&]() {
-    const int64_t ko = b * a.st[0] + h * a.st[1] + t * a.st[2], vo = b * a.st[3] + h * a.st[4] + t * a.st[5];
 #pragma unroll
     for (int e = 0; e < E; ++e) {
       const int c = min(lane + 64 * e, a.d - 1);
@@ -100,32 +111,36 @@ __global__ __launch_bounds__(256) void sfa_kv_append_q4_kernel(AppendQ4Args a) {
         nv[i][1] = ((const uint32_t*)a.v_new + vo)[c + 1];
       }
     }
-    int64_t page = -1, slot = 0;
     if (a.slots) {
-      const int s = __builtin_amdgcn_readfirstlane(a.slots[(int64_t)b * a.T + t]);
-      if (s >= 0 && s < a.num_pages * a.page_size) {  // (below 2^31)
-        page = a.log2P >= 0 ? s >> a.log2P : (uint32_t)s / (uint32_t)a.page_size;
-        slot = s - page * a.page_size;
-      }
+      nplace = a.slots[tok];
     } else {
-      const int c = a.n_new ? a.n_new[b] : a.T;
-      const int64_t pos = clamp_len(a.seq_len[b], cap) + t;
-      if (t < c && pos < cap) {
-        page = b;
-        slot = pos;
-        if (a.table) {
-          page = a.table[(int64_t)b * a.max_pages + (pos >> a.log2P)];
-          slot = pos & (a.page_size - 1);
-          if (page >= a.num_pages) page = -1;
-        }
+      if (b != len_of) {
+        len_of = b;
+        len = clamp_len(a.seq_len[b], cap);
+        if (a.n_new) count = a.n_new[b];
       }
+      npos = t < count ? len + t : cap;
+      nplace = a.table ? (npos < cap ? a.table[(int64_t)b * a.max_pages + (npos >> a.log2P)] : -1) : b;
     }
-    nrow = page < 0 ? -1 : (page * a.Hkv + h) * a.page_size + slot;
-    norow = ((int64_t)b * a.Hkv + h) * a.T + t;
+    norow = out_row;
   };
   load_row();
   while (true) {
-    const int64_t crow = nrow, orow = norow;
+    int64_t page, slot;
+    const int place = __builtin_amdgcn_readfirstlane(nplace);
+    bool kept;
+    if (a.slots) {
+      kept = place >= 0 && place < a.num_pages * a.page_size;  // (below 2^31)
+      page = a.log2P >= 0 ? place >> a.log2P : (uint32_t)place / (uint32_t)a.page_size;
+      slot = place - page * a.page_size;
+    } else {
+      kept = npos < cap && place >= 0 && place < a.num_pages;
+      page = place;
+      slot = a.table ? npos & (a.page_size - 1) : npos;
+    }
+    const int64_t crow = (page * a.Hkv + h) * a.page_size + slot, orow = norow;
+    // (the other arrays' offsets are shifts of these two)
+    const int64_t ck = crow * a.k, cv = crow * (a.d / 2);
     uint32_t bits[E], key[E], km = 0;
     float x[NV][2];
 #pragma unroll
@@ -143,17 +158,34 @@ __global__ __launch_bounds__(256) void sfa_kv_append_q4_kernel(AppendQ4Args a) {
     h += a.step_h;
     t += a.step_t;
     b += a.step_b;
-    if (h >= a.Hkv) { h -= a.Hkv; ++t; }
-    if (t >= a.T) { t -= a.T; ++b; }
+    ko += a.step_k;
+    vo += a.step_v;
+    tok += a.step_tok;
+    out_row += a.step_out;
+    if (h >= a.Hkv) {  // on to the next token
+      h -= a.Hkv;
+      ++t;
+      ko += a.carry_k;
+      vo += a.carry_v;
+      ++tok;
+      out_row += 1 - (int64_t)a.Hkv * a.T;
+    }
+    if (t >= a.T) {  // on to the next sequence
+      t -= a.T;
+      ++b;
+      ko += a.wrap_k;
+      vo += a.wrap_v;
+      out_row += (int64_t)(a.Hkv - 1) * a.T;
+    }
     const bool more = b < a.B;
     if (more) load_row();
-    if (crow >= 0) {  // uniform per wave
+    if (kept) {  // uniform per wave
       bool sel[E];
       topk_select<E>(key, a.k, sel);
       int sl[E];
       topk_slots<E>(sel, sl);
       // the kept values' largest magnitude is the row's: the largest key, |bits| + 1
-      const float ks = __uint_as_float(wave_umax(km) - 1u) / 7.f;
+      const float ks = seventh(__uint_as_float(wave_umax(km) - 1u));
       float kx[E], q[E];
 #pragma unroll
       for (int e = 0; e < E; ++e) kx[e] = sel[e] ? __uint_as_float(bits[e]) : 0.f;
@@ -165,8 +197,8 @@ __global__ __launch_bounds__(256) void sfa_kv_append_q4_kernel(AppendQ4Args a) {
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       for (int i = lane; i < a.k / 2; i += 64) {
         const uint32_t two = ((const uint32_t*)ent)[i];
-        ((uint16_t*)(a.kc_idx + crow * a.k))[i] = (uint16_t)((two & 255u) | ((two >> 8) & 0xff00u));
-        (a.kc_val + crow * (a.k / 2))[i] = (uint8_t)(((two >> 8) & 15u) | ((two >> 20) & 0xf0u));
+        ((uint16_t*)(a.kc_idx + ck))[i] = (uint16_t)((two & 255u) | ((two >> 8) & 0xff00u));
+        (a.kc_val + (ck >> 1))[i] = (uint8_t)(((two >> 8) & 15u) | ((two >> 20) & 0xf0u));
       }
       if (lane == 0) a.kc_scale[crow] = ks;
       if (a.k_idx)
@@ -181,13 +213,13 @@ __global__ __launch_bounds__(256) void sfa_kv_append_q4_kernel(AppendQ4Args a) {
       for (int i = 0; i < NV; ++i) {
         const int c = 2 * lane + 128 * i;
         const uint32_t m = row16_umax(max(__float_as_uint(x[i][0]) & 0x7fffffffu, __float_as_uint(x[i][1]) & 0x7fffffffu));
-        const uint32_t sb = f32_to_bf16_rne(__uint_as_float(m) / 7.f);
+        const uint32_t sb = f32_to_bf16_rne(seventh(__uint_as_float(m)));
         const float s = bf16_bits_to_f32(sb);
         float vq[2];
         quant4<2>(x[i], s, vq);
         if (c < a.d) {
-          (a.v_cache + crow * (a.d / 2))[c / 2] = (uint8_t)(((int)vq[0] & 15) | ((int)vq[1] & 15) << 4);
-          if ((lane & 15) == 0) a.v_scale[crow * groups + c / 32] = (uint16_t)sb;
+          (a.v_cache + cv)[c / 2] = (uint8_t)(((int)vq[0] & 15) | ((int)vq[1] & 15) << 4);
+          if ((lane & 15) == 0) a.v_scale[(cv >> 4) + c / 32] = (uint16_t)sb;
           if (a.v_out)
             *(uint32_t*)(a.v_out + orow * a.d + c) = f32_to_bf16_rne(vq[0] * s) | f32_to_bf16_rne(vq[1] * s) << 16;
         }
@@ -229,6 +261,15 @@ hipError_t launch_kv_append_q4(AppendQ4Args a, hipStream_t stream) {
     step /= a.Hkv;
     a.step_t = (int)(step % a.T);
     a.step_b = (int)(step / a.T);
+    // offsets of that step, and what a carry from heads to tokens, tokens to sequences adds
+    a.step_k = a.step_b * a.st[0] + a.step_h * a.st[1] + a.step_t * a.st[2];
+    a.step_v = a.step_b * a.st[3] + a.step_h * a.st[4] + a.step_t * a.st[5];
+    a.carry_k = a.st[2] - a.Hkv * a.st[1];
+    a.carry_v = a.st[5] - a.Hkv * a.st[4];
+    a.wrap_k = a.st[0] - a.T * a.st[2];
+    a.wrap_v = a.st[3] - a.T * a.st[5];
+    a.step_tok = (int64_t)a.step_b * a.T + a.step_t;
+    a.step_out = ((int64_t)a.step_b * a.Hkv + a.step_h) * a.T + a.step_t;
     const bool v2 = ((a.st[3] | a.st[4] | a.st[5]) & 1) == 0 && (uintptr_t)a.v_new % (a.vbf16 ? 4 : 8) == 0;
     if (a.kbf16) a.vbf16 ? launch_q4_t<true, true>(a, v2, grid, stream) : launch_q4_t<true, false>(a, v2, grid, stream);
     else a.vbf16 ? launch_q4_t<false, true>(a, v2, grid, stream) : launch_q4_t<false, false>(a, v2, grid, stream);

@@ -216,7 +216,9 @@ struct AppendQ4Args {
   int16_t* k_idx;
   float* k_val;
   uint16_t* v_out;
-  int log2P, step_h, step_t, step_b;  // set by the launcher
+  // set by the launcher
+  int log2P, step_h, step_t, step_b;
+  int64_t step_k, step_v, step_tok, step_out, carry_k, carry_v, wrap_k, wrap_v;
 };
 hipError_t launch_kv_append_q4(AppendQ4Args a, hipStream_t stream);
 // seq_len[b] += the appended count, clamped to the capacity (sfa_cache.hip)
