@@ -28,22 +28,36 @@ __device__ __forceinline__ uint32_t row16_umax(uint32_t x) {
 
 // N numbers of a row with scale s (uniform or not): round-half-even of the float32
 // quotient.  x * rcp(s) is off by less than 4 ulp, 2^-18 for the quotients here (at most
-// 7.1), so it rounds as the quotient does unless it lies within 2^-16 of a half; where
-// that happens, or the reciprocal leaves the normal range, the wavefront divides.
+// 7.1), so it rounds as the quotient does unless it lies within 2^-16 of a half h.
+// There x - h s, one fma, tells an exact tie (frequent where values and scales are
+// both bfloat16), which goes to the even number; only if some quotient is near a half
+// and not on it, or the reciprocal leaves the normal range, does the wavefront divide.
 template <int N>
 __device__ __forceinline__ void quant4(const float (&x)[N], float s, float (&q)[N]) {
   const float r = __builtin_amdgcn_rcpf(s);
-  bool near = s < 0x1p-100f;
-  float y[N];
+  const bool tiny = s < 0x1p-100f;
+  float off[N];
+  bool near = tiny;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    y[i] = x[i] * r;
-    q[i] = rintf(y[i]);
-    near |= fabsf(fabsf(y[i] - q[i]) - 0.5f) < 0x1p-16f;
+    const float y = x[i] * r;
+    q[i] = rintf(y);
+    off[i] = y - q[i];
+    near |= fabsf(off[i]) > 0.5f - 0x1p-16f;
   }
   if (wave_ballot(near)) {
+    bool unsure = tiny;
 #pragma unroll
-    for (int i = 0; i < N; ++i) q[i] = s > 0.f ? rintf(x[i] / s) : 0.f;
+    for (int i = 0; i < N; ++i) {
+      const float h = q[i] + copysignf(0.5f, off[i]), e = fmaf(-h, s, x[i]);
+      const bool at = fabsf(off[i]) > 0.5f - 0x1p-16f;
+      q[i] = at ? rintf(h) : q[i];
+      unsure |= at && e != 0.f;
+    }
+    if (wave_ballot(unsure)) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) q[i] = s > 0.f ? rintf(x[i] / s) : 0.f;
+    }
   }
 #pragma unroll
   for (int i = 0; i < N; ++i) q[i] = fminf(fmaxf(q[i], -7.f), 7.f);
@@ -195,14 +209,20 @@ __global__ __launch_bounds__(256) void sfa_kv_append_q4_kernel(AppendQ4Args a) {
         if (sel[e] && sl[e] < a.k) ent[sl[e]] = (uint16_t)((lane + 64 * e) | ((int)q[e] & 15) << 8);
       __builtin_amdgcn_wave_barrier();
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      for (int i = lane; i < a.k / 2; i += 64) {
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {  // (k <= d: at most 64 NV pairs)
+        const int i = lane + 64 * j;
+        if (i >= a.k / 2) break;
         const uint32_t two = ((const uint32_t*)ent)[i];
         ((uint16_t*)(a.kc_idx + ck))[i] = (uint16_t)((two & 255u) | ((two >> 8) & 0xff00u));
         (a.kc_val + (ck >> 1))[i] = (uint8_t)(((two >> 8) & 15u) | ((two >> 20) & 0xf0u));
       }
       if (lane == 0) a.kc_scale[crow] = ks;
       if (a.k_idx)
-        for (int i = lane; i < a.k; i += 64) {
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+          const int i = lane + 64 * j;
+          if (i >= a.k) break;
           const int v = ent[i];
           a.k_idx[orow * a.k + i] = (int16_t)(v & 255);
           a.k_val[orow * a.k + i] = (float)((int)((uint32_t)v << 20) >> 28) * ks;
