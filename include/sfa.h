@@ -684,7 +684,8 @@ size_t sfa_page_tables_workspace(int B);
  *          k_val go together.  Rows of tokens that are not written to the cache are
  *          left as they were.
  * Limits: d a multiple of 32, k a multiple of 8, k <= d <= 256 (SFA_ENOTSUP
- *         otherwise); B * Hkv * T <= 2^31; num_pages * page_size < 2^31;
+ *         otherwise); B * Hkv * T <= 2^31; num_pages * page_size and
+ *         num_pages * Hkv < 2^31;
  *         page_size a power of two with block_table (any with slots or a
  *         contiguous cache).
  * Errors: SFA_EINVAL, SFA_ENOTSUP, SFA_EHIP.

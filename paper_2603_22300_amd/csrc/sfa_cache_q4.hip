@@ -140,7 +140,7 @@ __global__ __launch_bounds__(256) void sfa_kv_append_q4_kernel(AppendQ4Args a) {
   };
   load_row();
   while (true) {
-    int64_t page, slot;
+    int page, slot;
     const int place = __builtin_amdgcn_readfirstlane(nplace);
     bool kept;
     if (a.slots) {
@@ -150,9 +150,10 @@ __global__ __launch_bounds__(256) void sfa_kv_append_q4_kernel(AppendQ4Args a) {
     } else {
       kept = npos < cap && place >= 0 && place < a.num_pages;
       page = place;
-      slot = a.table ? npos & (a.page_size - 1) : npos;
+      slot = (int)(a.table ? npos & (a.page_size - 1) : npos);
     }
-    const int64_t crow = (page * a.Hkv + h) * a.page_size + slot, orow = norow;
+    // (num_pages * Hkv < 2^31)
+    const int64_t crow = (int64_t)(page * a.Hkv + h) * a.page_size + slot, orow = norow;
     // (the other arrays' offsets are shifts of these two)
     const int64_t ck = crow * a.k, cv = crow * (a.d / 2);
     uint32_t bits[E], key[E], km = 0;

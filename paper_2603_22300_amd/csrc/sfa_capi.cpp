@@ -583,7 +583,7 @@ sfa_status sfa_kv_append_q4(const void* k_new, const void* v_new, const int64_t*
   if (!slots && !block_table && num_pages != B) return SFA_EINVAL;
   if (!is_val(k_new_t) || !is_val(v_new_t)) return SFA_EINVAL;
   if (d > 256 || d % 32 != 0 || k % 8 != 0) return SFA_ENOTSUP;
-  if ((long long)B * Hkv * T > (1LL << 31)) return SFA_ENOTSUP;
+  if ((long long)B * Hkv * T > (1LL << 31) || (long long)num_pages * Hkv > 0x7fffffffLL) return SFA_ENOTSUP;
   if (((uintptr_t)kc_idx | (uintptr_t)kc_val | (uintptr_t)v_cache | (uintptr_t)kc_scale) % 4 != 0 ||
       ((uintptr_t)v_scale | (uintptr_t)k_idx) % 2 != 0 || ((uintptr_t)k_val | (uintptr_t)v_out) % 4 != 0 ||
       (uintptr_t)k_new % (k_new_t == SFA_BF16 ? 2 : 4) != 0 || (uintptr_t)v_new % (v_new_t == SFA_BF16 ? 2 : 4) != 0)
