@@ -9,6 +9,7 @@ if libsfa.so is missing or the device is not a GPU, the call raises.
 from __future__ import annotations
 
 import ctypes
+import importlib.util
 import math
 import os
 
@@ -629,81 +630,42 @@ _PAIRINGS = {"halves": 0, "neighbours": 1}
 _ORDERS = {"sections": 0, "interleaved": 1, "own": 2}
 
 
-# The checks of this part are made of few and cheap calls (a step of one sequence is as
-# short as they are): get_device() says both whether a tensor is on a GPU and on which,
-# and what is wrong is only looked for once something is.
+# Checks and C calls of this part are native (_binding.so, csrc/sfa_binding.cpp): a step
+# of one sequence is as short as its checks.
 
-_S3, _S6 = ctypes.c_int64 * 3, ctypes.c_int64 * 6
-_U8, _I16, _BF16 = {torch.uint8: 0}, {torch.int16: 0}, {torch.bfloat16: SFA_BF16}
+_native = None
 
 
-def _launch(dev: int, name: str, *args):
-    """The C call on torch's current stream of GPU dev, with that device current."""
-    fn = getattr(_lib or lib(), name)
-    if torch._C._cuda_getDevice() == dev:
-        status = fn(*args, torch._C._cuda_getCurrentRawStream(dev))
-    else:
-        with torch.cuda.device(dev):
-            status = fn(*args, torch._C._cuda_getCurrentRawStream(dev))
-    if status != SFA_OK:
-        raise SfaError(status, name)
+def _binding():
+    """The native marshalling module, bound to libsfa.so's entry points."""
+    global _native
+    if _native is None:
+        path = os.path.join(_HERE, "_binding.so")
+        if not os.path.exists(path):
+            raise RuntimeError(f"{path} is missing: build it with `python -m paper_2603_22300_amd.build`")
+        spec = importlib.util.spec_from_file_location(__name__ + "._binding", path)
+        mod = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(mod)
+        L = lib()
+        mod.bind(*[ctypes.cast(f, ctypes.c_void_p).value for f in (
+            L.sfa_rope, L.sfa_rope_encode, L.sfa_rope_encode_bwd, L.sfa_page_tables,
+            L.sfa_kv_append_q4, L.sfa_attn_decode_q4)], torch._C._cuda_getCurrentRawStream)
+        _native = mod
+    return _native
 
 
-def _gpu(t, name: str) -> int:
-    """The GPU of a tensor."""
+def _tensor(t, name: str):
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
-    dev = t.get_device()
-    if dev < 0:
+    if not t.is_cuda:
         raise ValueError(f"{name} must be a GPU tensor (got {t.device})")
-    return dev
+    return t
 
 
-def _array(t, name: str, dtype, shape, dev: int) -> int:
-    """The address of a contiguous tensor of that dtype and shape (None: any) on GPU dev."""
-    if isinstance(t, torch.Tensor) and t.get_device() == dev and t.dtype is dtype \
-            and (shape is None or t.shape == shape) and t.is_contiguous():
-        return t.data_ptr()
-    _gpu(t, name)
-    if t.dtype is not dtype:
-        raise TypeError(f"{name}: unsupported dtype {t.dtype} (wants {dtype})")
-    if t.get_device() != dev:
-        raise ValueError(f"{name} is on {t.device}, not on GPU {dev}")
-    if shape is not None and t.shape != shape:
-        raise ValueError(f"{name} must be {list(shape)} (got {list(t.shape)})")
-    raise ValueError(f"{name} must be contiguous")
-
-
-def _code(t, name: str, table) -> int:
-    code = table.get(t.dtype)
-    if code is None:
-        raise TypeError(f"{name}: unsupported dtype {t.dtype}")
-    return code
-
-
-def _rows4(t, name: str, shape, dev: int):
-    """Address, dtype code and strides (batch, head, token; None: contiguous) of float32
-    or bf16 rows [B, H, n, d] on GPU dev, any strides with contiguous coordinates."""
-    if not isinstance(t, torch.Tensor) or t.get_device() != dev:
-        _gpu(t, name)
-        raise ValueError(f"{name} is on {t.device}, not on GPU {dev}")
-    code = _code(t, name, _VAL)
-    if t.shape != shape:
-        raise ValueError(f"{name} must be {list(shape)} (got {list(t.shape)})")
-    if t.is_contiguous():
-        return t.data_ptr(), code, None
-    st = t.stride()
-    if st[3] != 1 and shape[3] != 1:
-        raise ValueError(f"{name}: a row's coordinates must be contiguous")
-    return t.data_ptr(), code, _S3(st[0], st[1], st[2])
-
-
-def _heads(t, name: str):
-    """GPU and shape of a [B, H, n, d] tensor."""
-    dev = _gpu(t, name)
-    if t.dim() != 4:
-        raise ValueError(f"{name} must be [B, H, n, d]")
-    return dev, t.shape
+def _plan(plan) -> int:
+    if type(plan) is not RopePlan:
+        raise TypeError("plan must come from sfa_rope_plan")
+    return plan._at
 
 
 class RopePlan:
@@ -716,6 +678,7 @@ class RopePlan:
         _call(lib().sfa_rope_plan_init(ctypes.byref(self._c), d, sec, len(sections), float(theta),
                                        pairing, order), "sfa_rope_plan_init")
         self.ref = ctypes.byref(self._c)
+        self._at = ctypes.addressof(self._c)
 
     d = property(lambda self: self._c.d)
     rot = property(lambda self: self._c.rot)
@@ -740,42 +703,16 @@ def sfa_rope_plan(d: int, sections=None, theta: float = 10000.0, pairing: str = 
                     _PAIRINGS[pairing], _ORDERS[order])
 
 
-def _pos(pos, plan, dev, B, n):
-    """Position tensor [naxes, B, n], [B, n] or [n] (int32, tokens contiguous; entries of
-    size 1 are shared): its address and its axis and batch strides."""
-    if not isinstance(plan, RopePlan):
-        raise TypeError("plan must come from sfa_rope_plan")
-    if not isinstance(pos, torch.Tensor) or pos.dtype is not torch.int32:
-        raise TypeError("pos must be an int32 tensor")
-    if pos.get_device() != dev:
-        raise ValueError(f"pos is on {pos.device}, not on GPU {dev}")
-    shape, st = pos.shape, pos.stride()
-    if len(shape) < 3:
-        shape, st = (1,) * (3 - len(shape)) + tuple(shape), (0,) * (3 - len(shape)) + st
-    if len(shape) != 3 or shape[0] not in (1, plan._c.naxes) or shape[1] not in (1, B) or shape[2] != n:
-        raise ValueError("pos must be [naxes, B, n], [B, n] or [n]")
-    if n > 1 and st[2] != 1:
-        raise ValueError("pos: tokens must be contiguous")
-    return pos.data_ptr(), st[0] if shape[0] > 1 else 0, st[1] if shape[1] > 1 else 0
-
-
 def sfa_rope(x, pos, plan: RopePlan, inverse: bool = False, y_dtype=None,
              y: torch.Tensor | None = None):
     """Rotary positions on x [B, H, n, d] (float32 or bf16; any strides with
     contiguous coordinates): y of y_dtype (default x's), or into the caller's y
     (which may be x).  inverse=True turns back: the gradient of the rotation."""
-    dev, shape = _heads(x, "x")
-    B, H, n, d = shape
-    pp, pa, pb = _pos(pos, plan, dev, B, n)
-    if d != plan._c.d:
-        raise ValueError(f"x has {d} coordinates, the plan {plan.d}")
-    xp, xt, xs = _rows4(x, "x", shape, dev)
     if y is None:
-        y = torch.empty(shape, dtype=y_dtype or x.dtype, device=x.device)
-    yp, yt, ys = _rows4(y, "y", shape, dev)
-    if B and H and n:
-        _launch(dev, "sfa_rope", xp, xs, pp, pa, pb, plan.ref, B, H, n, 1 if inverse else 0, xt, yt,
-                yp, ys)
+        y = torch.empty(_tensor(x, "x").shape, dtype=y_dtype or x.dtype, device=x.device)
+    status = (_native or _binding()).rope(x, pos, _plan(plan), bool(inverse), y)
+    if status:
+        raise SfaError(status, "sfa_rope")
     return y
 
 
@@ -783,21 +720,13 @@ def sfa_rope_encode(x, pos, plan: RopePlan, k: int, idx_dtype=torch.int32, val_d
                     idx: torch.Tensor | None = None, val: torch.Tensor | None = None):
     """Top-k codes of the rotated rows of x [B, H, n, d] in one pass: (idx, val)
     [B, H, n, k], as sfa_topk_encode of sfa_rope's float32 rows."""
-    dev, shape = _heads(x, "x")
-    B, H, n, d = shape
-    pp, pa, pb = _pos(pos, plan, dev, B, n)
-    if d != plan._c.d:
-        raise ValueError(f"x has {d} coordinates, the plan {plan.d}")
-    xp, xt, xs = _rows4(x, "x", shape, dev)
-    if idx is None:
-        idx = torch.empty((B, H, n, k), dtype=idx_dtype, device=x.device)
-    if val is None:
-        val = torch.empty((B, H, n, k), dtype=val_dtype, device=x.device)
-    it, vt = _code(idx, "idx", _IDX), _code(val, "val", _CVAL)
-    ip = _array(idx, "idx", idx.dtype, (B, H, n, k), dev)
-    vp = _array(val, "val", val.dtype, (B, H, n, k), dev)
-    if B and H and n:
-        _launch(dev, "sfa_rope_encode", xp, xs, pp, pa, pb, plan.ref, B, H, n, k, xt, ip, it, vp, vt)
+    if idx is None or val is None:
+        shape = _tensor(x, "x").shape[:-1] + (k,)
+        idx = torch.empty(shape, dtype=idx_dtype, device=x.device) if idx is None else idx
+        val = torch.empty(shape, dtype=val_dtype, device=x.device) if val is None else val
+    status = (_native or _binding()).rope_encode(x, pos, _plan(plan), k, idx, val)
+    if status:
+        raise SfaError(status, "sfa_rope_encode")
     return idx, val
 
 
@@ -807,17 +736,12 @@ def sfa_rope_encode_bwd(idx, dval, pos, plan: RopePlan, dx_dtype=torch.float32,
     float32 of the code values, at idx [B, H, n, k], turned back into dx [B, H, n, d]
     (dx_dtype, or the caller's dx: float32 or bf16, any strides with contiguous
     coordinates, every coordinate written)."""
-    dev, code = _heads(idx, "idx")
-    B, H, n, k = code
-    pp, pa, pb = _pos(pos, plan, dev, B, n)
-    it = _code(idx, "idx", _IDX)
-    ip, gp = _array(idx, "idx", idx.dtype, None, dev), _array(dval, "dval", torch.float32, code, dev)
-    shape = (B, H, n, plan._c.d)
+    at = _plan(plan)
     if dx is None:
-        dx = torch.empty(shape, dtype=dx_dtype, device=idx.device)
-    xp, xt, xs = _rows4(dx, "dx", shape, dev)
-    if B and H and n:
-        _launch(dev, "sfa_rope_encode_bwd", ip, it, gp, pp, pa, pb, plan.ref, B, H, n, k, xt, xp, xs)
+        dx = torch.empty(_tensor(idx, "idx").shape[:-1] + (plan.d,), dtype=dx_dtype, device=idx.device)
+    status = (_native or _binding()).rope_encode_bwd(idx, dval, pos, at, dx)
+    if status:
+        raise SfaError(status, "sfa_rope_encode_bwd")
     return dx
 
 
@@ -843,57 +767,28 @@ def sfa_page_tables(old_len, new_len, block_table, free_pages, free_in, page_siz
     Returns (got, free_out, starts, slots, pos): the lengths that the pages reached
     [B], the new free count [1], the first row of each sequence [B + 1], and the maps
     (or None)."""
-    i32, dev = torch.int32, _gpu(new_len, "new_len")
-    B = new_len.numel()
-    np_ = _array(new_len, "new_len", i32, None, dev)
-    op = _i32_of(old_len, "old_len", B, dev) if old_len is not None else 0
-    if not isinstance(block_table, torch.Tensor) or block_table.dim() != 2 or block_table.shape[0] != B:
-        raise ValueError("block_table must be [B, max_pages]")
-    tp, fp = _array(block_table, "block_table", i32, None, dev), _array(free_pages, "free_pages", i32, None, dev)
-    new = dict(dtype=i32, device=new_len.device)
-    free_out = torch.empty((1,), **new) if free_out is None else free_out
-    got = torch.empty((B,), **new) if got is None else got
-    starts = torch.empty((B + 1,), **new) if starts is None else starts
-    if slots is None and pos is None and n_rows > 0:
-        slots, pos = torch.empty((n_rows,), **new), torch.empty((n_rows,), **new)
-    rows = slots.numel() if slots is not None else pos.numel() if pos is not None else 0
-    sp = _i32_of(slots, "slots", rows, dev) if slots is not None else 0
-    pp = _i32_of(pos, "pos", rows, dev) if pos is not None else 0
-    if ws is None:
-        ws = torch.empty(sfa_page_tables_workspace(B), dtype=torch.uint8, device=new_len.device)
-    _launch(dev, "sfa_page_tables", op, np_, B, tp, block_table.shape[1], page_size, fp, free_pages.numel(),
-            _i32_of(free_in, "free_in", 1, dev), _i32_of(free_out, "free_out", 1, dev),
-            _i32_of(got, "got", B, dev), _i32_of(starts, "starts", B + 1, dev), sp, pp, rows,
-            _array(ws, "ws", ws.dtype, None, dev), ws.nbytes)
+    new = None
+    if free_out is None or got is None or starts is None or ws is None \
+            or (n_rows > 0 and slots is None and pos is None):
+        B = _tensor(new_len, "new_len").numel()
+        new = dict(dtype=torch.int32, device=new_len.device)
+        free_out = torch.empty((1,), **new) if free_out is None else free_out
+        got = torch.empty((B,), **new) if got is None else got
+        starts = torch.empty((B + 1,), **new) if starts is None else starts
+        if slots is None and pos is None and n_rows > 0:
+            slots, pos = torch.empty((n_rows,), **new), torch.empty((n_rows,), **new)
+        if ws is None:
+            ws = torch.empty(sfa_page_tables_workspace(B), dtype=torch.uint8, device=new_len.device)
+    status = (_native or _binding()).page_tables(old_len, new_len, block_table, free_pages, free_in, page_size,
+                                                 free_out, got, starts, slots, pos, ws)
+    if status:
+        raise SfaError(status, "sfa_page_tables")
     return got, free_out, starts, slots, pos
-
-
-def _i32_of(t, name: str, n: int, dev: int) -> int:
-    p = _array(t, name, torch.int32, None, dev)
-    if t.numel() != n:
-        raise ValueError(f"{name} must hold {n} entries")
-    return p
 
 
 # ---------------------------------------------------------------------------
 # 4-bit cache
 # ---------------------------------------------------------------------------
-
-def _q4_cache(kc_idx, kc_val, kc_scale, v_cache, v_scale):
-    """Checks the five arrays of a 4-bit cache; returns the GPU, (pages, Hkv, page_size,
-    k, d) and the addresses."""
-    dev, u8 = _gpu(kc_idx, "kc_idx"), torch.uint8
-    _gpu(v_cache, "v_cache")
-    if kc_idx.dim() != 4 or v_cache.dim() != 4:
-        raise ValueError("kc_idx must be [pages, Hkv, page_size, k], v_cache [pages, Hkv, page_size, d / 2]")
-    N, H, P, k = kc_idx.shape
-    d2 = v_cache.shape[3]
-    return dev, (N, H, P, k, 2 * d2), (
-        _array(kc_idx, "kc_idx", u8, None, dev), _array(kc_val, "kc_val", u8, (N, H, P, k // 2), dev),
-        _array(kc_scale, "kc_scale", torch.float32, (N, H, P), dev),
-        _array(v_cache, "v_cache", u8, (N, H, P, d2), dev),
-        _array(v_scale, "v_scale", torch.bfloat16, (N, H, P, d2 // 16), dev))
-
 
 def sfa_kv_append_q4(k_new, v_new, seq_len, kc_idx, kc_val, kc_scale, v_cache, v_scale, k: int,
                      block_table=None, n_new=None, slots=None, k_idx=None, k_val=None, v_out=None):
@@ -906,42 +801,11 @@ def sfa_kv_append_q4(k_new, v_new, seq_len, kc_idx, kc_val, kc_scale, v_cache, v
     seq_len None and slots [B, T] int32 (as sfa_page_tables writes them; rows outside
     the pool are skipped).  k_idx int16 and k_val float32 [B, Hkv, T, k], v_out bf16
     [B, Hkv, T, d]: if given, the numbers the cache now stands for."""
-    dev, (pages, hkv, P, kc, dc), cache = _q4_cache(kc_idx, kc_val, kc_scale, v_cache, v_scale)
-    shape = _heads(k_new, "k_new")[1]
-    B, Hkv, T, d = shape
-    kp, kt, kst = _rows4(k_new, "k_new", shape, dev)
-    vp, vt, vst = _rows4(v_new, "v_new", shape, dev)
-    if hkv != Hkv or kc != k or dc != d:
-        raise ValueError("the cache's heads, k or d are not those of k_new")
-    st = None
-    if kst is not None or vst is not None:
-        st = _S6(*(kst or (Hkv * T * d, T * d, d)), *(vst or (Hkv * T * d, T * d, d)))
-    sp = lp = np_ = tp = maxp = 0
-    if slots is not None:
-        if seq_len is not None or n_new is not None or block_table is not None:
-            raise ValueError("slots say where every token goes: give no seq_len, n_new or block_table")
-        sp = _i32_of(slots, "slots", B * T, dev)
-    else:
-        lp = _i32_of(seq_len, "seq_len", B, dev)
-        np_ = _i32_of(n_new, "n_new", B, dev) if n_new is not None else 0
-        if block_table is not None:
-            tp, maxp = _table(block_table, B, dev)
-        elif pages != B:
-            raise ValueError("a contiguous cache holds B sequences")
-    code = (B, Hkv, T, k)
-    ip = _array(k_idx, "k_idx", torch.int16, code, dev) if k_idx is not None else 0
-    qp = _array(k_val, "k_val", torch.float32, code, dev) if k_val is not None else 0
-    op = _array(v_out, "v_out", torch.bfloat16, shape, dev) if v_out is not None else 0
-    _launch(dev, "sfa_kv_append_q4", kp, vp, st, sp, np_, lp, B, Hkv, T, d, k, tp, maxp, P, pages,
-            *cache, ip, qp, op, kt, vt)
+    status = (_native or _binding()).kv_append_q4(kc_idx, kc_val, kc_scale, v_cache, v_scale, k_new, v_new, k,
+                                                  seq_len, n_new, block_table, slots, k_idx, k_val, v_out)
+    if status:
+        raise SfaError(status, "sfa_kv_append_q4")
     return seq_len
-
-
-def _table(block_table, B: int, dev: int):
-    p = _array(block_table, "block_table", torch.int32, None, dev)
-    if block_table.dim() != 2 or block_table.shape[0] != B:
-        raise ValueError("block_table must be [B, max_pages]")
-    return p, block_table.shape[1]
 
 
 def sfa_attn_decode_q4_workspace(B: int, Hq: int, Lmax: int, d: int) -> int:
@@ -956,43 +820,18 @@ def sfa_attn_decode_q4(kc_idx, kc_val, kc_scale, v_cache, v_scale, block_table=N
     """Decode over a 4-bit cache (contiguous, or paged with block_table), with query
     codes q_idx / q_val [B, Hq, k] or a dense float32 query q [B, Hq, d] coded in the
     kernel.  Returns (o [B, Hq, d], lse [B, Hq] or None)."""
-    dev, (pages, Hkv, P, k, d), cache = _q4_cache(kc_idx, kc_val, kc_scale, v_cache, v_scale)
-    qp = qip = qvp = qit = qvt = 0
-    if q is not None:
-        if q_idx is not None or q_val is not None:
-            raise ValueError("give either q or (q_idx, q_val)")
-        qp = _array(q, "q", torch.float32, None, dev)
-        if q.dim() != 3 or q.shape[2] != d:
-            raise ValueError("q must be [B, Hq, d]")
-        B, Hq, _ = q.shape
-    else:
-        _gpu(q_idx, "q_idx"); _gpu(q_val, "q_val")
-        qit, qvt = _code(q_idx, "q_idx", _IDX), _code(q_val, "q_val", _CVAL)
-        if q_idx.dim() != 3 or q_idx.shape[2] != k:
-            raise ValueError("q codes must be [B, Hq, k]")
-        B, Hq, _ = q_idx.shape
-        qip = _array(q_idx, "q_idx", q_idx.dtype, None, dev)
-        qvp = _array(q_val, "q_val", q_val.dtype, (B, Hq, k), dev)
-    tp, maxp, cap = 0, 0, P
-    if block_table is not None:
-        tp, maxp = _table(block_table, B, dev)
-        cap = maxp * P
-    elif pages != B:
-        raise ValueError("a contiguous cache holds B sequences")
-    sp = _i32_of(seq_len, "seq_len", B, dev) if seq_len is not None else 0
-    if scale is None:
-        scale = d ** -0.5
-    if o is None:
-        o = torch.empty((B, Hq, d), dtype=o_dtype, device=v_cache.device)
-    op, ot = _array(o, "o", o.dtype, (B, Hq, d), dev), _code(o, "o", _VAL)
-    if lse is None and want_lse:
-        lse = torch.empty((B, Hq), dtype=torch.float32, device=v_cache.device)
-    ep = _array(lse, "lse", torch.float32, None, dev) if lse is not None else 0
-    if ep and lse.numel() != B * Hq:
-        raise ValueError("lse must hold B * Hq entries")
-    if ws is None:
-        ws = torch.empty(sfa_attn_decode_q4_workspace(B, Hq, cap, d), dtype=torch.uint8,
-                         device=v_cache.device)
-    _launch(dev, "sfa_attn_decode_q4", qp, qip, qvp, *cache, tp, maxp, P, pages, sp, B, Hq, Hkv, d, k, scale,
-            window, n_global, qit, qvt, ot, op, ep, _array(ws, "ws", ws.dtype, None, dev), ws.nbytes)
+    if o is None or (lse is None and want_lse) or ws is None:
+        B, Hq = _tensor(q if q is not None else q_idx, "q" if q is not None else "q_idx").shape[:2]
+        d, P = 2 * _tensor(v_cache, "v_cache").shape[-1], v_cache.shape[2]
+        if o is None:
+            o = torch.empty((B, Hq, d), dtype=o_dtype, device=v_cache.device)
+        if lse is None and want_lse:
+            lse = torch.empty((B, Hq), dtype=torch.float32, device=v_cache.device)
+        if ws is None:
+            cap = P if block_table is None else _tensor(block_table, "block_table").shape[-1] * P
+            ws = torch.empty(sfa_attn_decode_q4_workspace(B, Hq, cap, d), dtype=torch.uint8, device=v_cache.device)
+    status = (_native or _binding()).attn_decode_q4(kc_idx, kc_val, kc_scale, v_cache, v_scale, block_table, seq_len,
+                                                    q, q_idx, q_val, scale, o, lse, ws, window, n_global)
+    if status:
+        raise SfaError(status, "sfa_attn_decode_q4")
     return o, lse
