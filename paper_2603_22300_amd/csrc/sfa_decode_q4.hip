@@ -8,52 +8,52 @@
 //   scores   lane = key.  s_h = scale * ks * sum_t q4_t * qd[u_t][h], qd the dense
 //            query rows in LDS; float32.
 //   softmax  base 2, online, the running maximum kept uniform over the wavefront.
-//   P.V      on the matrix cores, v_mfma_f32_16x16x32_f16.  The weights of a group
-//            of 32 coordinates are p * vs, split into two float16 pieces, p0 =
-//            f16(p vs) and p1 = f16(p vs - p0): the pieces of the group's query
-//            heads fill the sixteen rows of one operand, so the second piece (and
-//            with it float32 accuracy, 2^-22) costs no matrix instruction.  The
-//            other operand is the cached numbers: a nibble with its sign flipped is
-//            q + 8, and set into the low mantissa bits of a float16 it is (q + 8)
-//            2^-24, or 16 times that at bit 4 (odd keys; their weights carry 1/16):
-//            subnormal numbers, which the matrix cores keep.  One instruction per
-//            two numbers; a second matrix instruction with a constant operand takes
-//            the 8 off again, block by block, so that the sums stay small.
-// Both operands have 16 or 8 keys of one row in a lane, and both are held key by
-// key: the transposing LDS reads turn them, ds_read_b64_tr_b4 the cached nibbles
-// as they are and ds_read_b64_tr_b16 the weights.  Value rows are loaded a block of
+//   P.V      on the matrix cores, v_mfma_i32_16x16x64_i8, in whole numbers.  The
+//            weights of a group of 32 coordinates, p * vs, are rounded to whole numbers
+//            of 32 bits and written as four digits of a signed byte: four query heads'
+//            digits are the sixteen rows of one operand, a lane of the result holds the
+//            four digits' sums of one head.  The other operand is the cached nibbles as
+//            they are, at the high end of a byte: 16 q.  Products and sums are exact
+//            (1024 keys at most to a wavefront, 2^24); what is lost is the weights'
+//            rounding alone, 2^-29 of the largest p times the group's largest value scale.
+// Both operands have 16 keys of one row in a lane, and both are held key by key: the
+// transposing LDS reads turn them, ds_read_b64_tr_b4 the cached nibbles and
+// ds_read_b64_tr_b8 the weights.  Value rows are loaded a block of
 // keys ahead and written to LDS with the 16-byte pieces of a row exchanged, so that the
 // transposing reads find each key on banks of its own.  (Through registers: with
 // loads sent to LDS directly, the compiler waits for them at every later LDS read.)
 //
-// float16 range: each group's weights are scaled by a power of two that follows
-// the largest value scale seen in the group, as the running maximum does for p
-// (`vexp` below): value scales from 2^-116 up keep their accuracy.  Both follow
-// lazily, p up to 2^4 and only upwards for the scales, so that most blocks of keys
-// touch neither the maxima nor the accumulators.
+// Range: each group's weights are scaled by a power of two that follows the largest
+// value scale seen in the group, as the running maximum does for p (`vexp` below).  Both
+// follow lazily, p up to 2^1.9 and only upwards for the scales, so that most blocks of
+// keys touch neither the maxima nor the sums.
 #include "sfa_decode_kernel.h"
 
 namespace sfa {
 namespace {
 
 typedef int v2i __attribute__((ext_vector_type(2)));
-typedef short v4s __attribute__((ext_vector_type(4)));
-typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef int v4i __attribute__((ext_vector_type(4)));
 
 __device__ __forceinline__ v2i read_tr4(const void* p) {
   return __builtin_amdgcn_ds_read_tr4_b64_v2i32((__attribute__((address_space(3))) v2i*)p);
 }
-__device__ __forceinline__ v4s read_tr16(const void* p) {
-  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)p);
+__device__ __forceinline__ v2i read_tr8(const void* p) {
+  return __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) v2i*)p);
 }
 
-// Eight nibbles (two's complement), each as (q + 8) 2^-24 in float16, those of odd
-// keys 16 times that, in the order n0 n4 n1 n5 n2 n6 n3 n7.
-__device__ __forceinline__ f16x8 nibbles_f16(uint32_t x) {
-  const uint32_t y = x >> 8;
-  const u32x4 r = {(x & 0x000f000fu) ^ 0x00080008u, (x & 0x00f000f0u) ^ 0x00800080u,
-                   (y & 0x000f000fu) ^ 0x00080008u, (y & 0x00f000f0u) ^ 0x00800080u};
-  return __builtin_bit_cast(f16x8, r);
+// Sixteen nibbles q (two's complement) as bytes 16 q, in the order 0 2 4 6, 1 3 5 7 of
+// each eight.
+__device__ __forceinline__ v4i nibbles_i8(v2i x) {
+  return v4i{(int)((uint32_t)x.x << 4 & 0xf0f0f0f0u), (int)(x.x & 0xf0f0f0f0u),
+             (int)((uint32_t)x.y << 4 & 0xf0f0f0f0u), (int)(x.y & 0xf0f0f0f0u)};
+}
+
+// A whole number w as digits to the base 256, -128 to 127 each (|w| < 2^30.99).
+__device__ __forceinline__ uint32_t digits(int w) { return ((uint32_t)w + 0x80808080u) ^ 0x80808080u; }
+// ... and the number that four sums of digits stand for (each |sum| < 2^25).
+__device__ __forceinline__ float from_digits(v4i a) {
+  return fmaf((float)a[3], 0x1p24f, fmaf((float)a[2], 0x1p16f, fmaf((float)a[1], 0x1p8f, (float)a[0])));
 }
 
 __device__ __forceinline__ float pow2_field(int field) { return __uint_as_float((uint32_t)field << 23); }
@@ -84,7 +84,7 @@ void sfa_decode_q4_kernel(DecParams p, int dd, const uint16_t* vscale) {
   const int k = KC8 > 0 ? 8 * KC8 : p.k;
   __shared__ float qd[256][GP];  // (an index past d reads zeros)
   __shared__ __attribute__((aligned(16))) unsigned char vt[kDecWaves][64 * D / 2];
-  __shared__ __attribute__((aligned(16))) _Float16 pb[kDecWaves][NG][64][2 * GP];
+  __shared__ __attribute__((aligned(16))) uint32_t pb[kDecWaves][NG][64][GP];  // digits of the weights
   __shared__ float red_m[kDecWaves][GP], red_l[kDecWaves][GP];
 
   const int tid = threadIdx.x, lane = tid & 63;
@@ -120,19 +120,17 @@ void sfa_decode_q4_kernel(DecParams p, int dd, const uint16_t* vscale) {
   float m_run[GP], m_use[GP], l_lane[GP];  // m_use: m_run, or 0 before the first key
 #pragma unroll
   for (int h = 0; h < GP; ++h) { m_run[h] = -INFINITY; m_use[h] = 0.f; l_lane[h] = 0.f; }
-  floatx4 acc[2 * NG];
+  constexpr int NS = GP / 4;  // operands of four heads
+  v4i acc[NS][2 * NG];
 #pragma unroll
-  for (int t = 0; t < 2 * NG; ++t) acc[t] = floatx4{0.f, 0.f, 0.f, 0.f};
-  // Per group, the exponent field of the largest value scale seen, at least 11; the
-  // weights of even keys carry 2^(137 - vexp): a scale of that exponent field becomes
-  // 2^10 to 2^11 and a weight at most 2^15, and the smallest weight that the second
-  // piece still holds is 2^-34 of p = 1 (2^-30 for odd keys).
+  for (int t = 0; t < NS * 2 * NG; ++t) acc[t / (2 * NG)][t % (2 * NG)] = v4i{0, 0, 0, 0};
+  // Per group, the exponent field of the largest value scale seen, at least 1 (255: an
+  // infinity or NaN).  Weights carry 2^(155 - vexp): p = 1 with a scale of that field
+  // becomes 2^28 to 2^29, and the largest weight is less than 2^30.9.
   int vexp[NG];
-  float vpow[NG];  // that power of two, this lane's key's
-  const int odd4 = 4 * (lane & 1);
 #pragma unroll
-  for (int g = 0; g < NG; ++g) { vexp[g] = 11; vpow[g] = pow2_field(264 - 11 - odd4); }
-  float pass = -INFINITY;  // exponents past it raise the maxima: 2^4 once there are any
+  for (int g = 0; g < NG; ++g) vexp[g] = 1;
+  float pass = -INFINITY;  // exponents past it raise the maxima: 2^1.9 once there are any
 
   const int64_t kv_row0 = ((int64_t)b * p.Hkv + hkv) * p.Lmax;
   const int per_wave = plan.c / kDecWaves;
@@ -234,12 +232,17 @@ void sfa_decode_q4_kernel(DecParams p, int dd, const uint16_t* vscale) {
   };
   // operand addresses in LDS
   const int r16 = lane & 15, key0 = lane & 48;
-  const _Float16* a_src = &pb[wave][0][key0 + (r16 >> 3) + 4 * ((r16 >> 2) & 1)][4 * ((r16 & 3) & (GP / 2 - 1))];
+  // weights: a key's place in its group's block (each odd sixteen keys have their halves
+  // exchanged, so that the reads of a half of each sixteen fall on all banks)
+  auto place = [](int key) { return key ^ (key >> 1 & 8); };
+  const int ak = r16 >> 1;  // key ak of eight in the nibbles' order
+  const uint32_t* a_src[2];
+#pragma unroll
+  for (int m = 0; m < 2; ++m) a_src[m] = &pb[wave][0][place(key0 + 8 * m + (2 * ak & 6) + (ak >> 2))][2 * (r16 & 1)];
   const unsigned char* b_src[NG];
 #pragma unroll
   for (int g = 0; g < NG; ++g)
     b_src[g] = vw + (key0 + r16) * (d / 2) + (g ^ ((r16 >> sw_shift) & sw_mask)) * 16;
-  const u32x4 minus8 = {0x80088008u, 0x80808080u, 0x80088008u, 0x80808080u};
 
   int page = 0;
   if (w0 < w1) {
@@ -326,7 +329,7 @@ void sfa_decode_q4_kernel(DecParams p, int dd, const uint16_t* vscale) {
 #pragma unroll
       for (int g = 0; g < NG; ++g) vs[g] = ok ? vs[g] : 0u;
     }
-    // a key that passes a running maximum by 2^4, or a group's exponent
+    // a key that passes a running maximum by 2^1.9, or a group's exponent
     float tmax = t[0];
 #pragma unroll
     for (int h = 1; h < GP; ++h) tmax = fmaxf(tmax, t[h]);
@@ -334,7 +337,7 @@ void sfa_decode_q4_kernel(DecParams p, int dd, const uint16_t* vscale) {
 #pragma unroll
     for (int g = 0; g < NG; ++g) up |= wave_ballot(vs[g] > (uint32_t)(vexp[g] << 23 | 0x7fffff));
     if (up) {  // uniform; the first block always
-      float fa[4];
+      float fa[NS];
       {
         float alpha[GP];
 #pragma unroll
@@ -347,20 +350,25 @@ void sfa_decode_q4_kernel(DecParams p, int dd, const uint16_t* vscale) {
           m_use[h] = m_new == -INFINITY ? 0.f : m_new;
           t[h] = x - m_use[h];
         }
-        pass = m_run[0] == -INFINITY ? -INFINITY : 4.f;
+        pass = m_run[0] == -INFINITY ? -INFINITY : 1.9f;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) fa[i] = GP == 4 || !(lane & 16) ? alpha[i] : alpha[GP - 4 + i];
+        for (int n = 0; n < NS; ++n) {  // this lane's head of the four
+          const float lo = lane & 16 ? alpha[4 * n + 1] : alpha[4 * n];
+          const float hi = lane & 16 ? alpha[4 * n + 3] : alpha[4 * n + 2];
+          fa[n] = lane & 32 ? hi : lo;
+        }
       }
 #pragma unroll
       for (int g = 0; g < NG; ++g) {
-        const int vnew = max(vexp[g], min((int)(wave_umax(vs[g] & 0x7fffffffu) >> 23), 254));
+        const int vnew = max(vexp[g], (int)(wave_umax(vs[g] & 0x7fffffffu) >> 23));
         const float f = vnew - vexp[g] > 126 ? 0.f : pow2_field(127 + vexp[g] - vnew);
         vexp[g] = vnew;
-        vpow[g] = pow2_field(264 - vnew - odd4);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          acc[2 * g][i] *= f * fa[i];
-          acc[2 * g + 1][i] *= f * fa[i];
+        for (int t = 0; t < NS * 2; ++t) {  // rounded to 24 bits, kept as two digits
+          v4i& a = acc[t / 2][2 * g + t % 2];
+          const float v = from_digits(a) * (f * fa[t / 2]);
+          const float top = rintf(v * 0x1p-24f);
+          a = v4i{(int)rintf(fmaf(top, -0x1p24f, v)), 0, 0, (int)top};
         }
       }
     }
@@ -370,44 +378,36 @@ void sfa_decode_q4_kernel(DecParams p, int dd, const uint16_t* vscale) {
       pj[h] = __builtin_amdgcn_exp2f(t[h]);
       l_lane[h] += pj[h];
     }
-    // weights: [group][key][pieces 0 of the heads, pieces 1]
+    // weights, rounded to the nearest whole number
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
       if (g >= ng) break;
-      const float f = __uint_as_float(vs[g]) * vpow[g];
-      f16x8 w[GP / 4];
+      const float f = __builtin_ldexpf(__uint_as_float(vs[g]), 155 - vexp[g]);
 #pragma unroll
-      for (int h = 0; h < GP; h += 2) {
-        const auto x0 = __builtin_amdgcn_cvt_pkrtz(pj[h] * f, pj[h + 1] * f);
-        w[h / 8][h % 8] = (_Float16)x0[0];
-        w[h / 8][h % 8 + 1] = (_Float16)x0[1];
-        w[(GP + h) / 8][(GP + h) % 8] = (_Float16)fmaf(pj[h], f, -(float)x0[0]);
-        w[(GP + h) / 8][(GP + h) % 8 + 1] = (_Float16)fmaf(pj[h + 1], f, -(float)x0[1]);
+      for (int n = 0; n < NS; ++n) {
+        u32x4 w;
+#pragma unroll
+        for (int h = 0; h < 4; ++h) w[h] = digits((int)fmaf(pj[4 * n + h], f, 0.5f));
+        *(u32x4*)&pb[wave][g][place(lane)][4 * n] = w;
       }
-#pragma unroll
-      for (int i = 0; i < GP / 4; ++i) ((f16x8*)&pb[wave][g][lane][0])[i] = w[i];
     }
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_sched_barrier(0);
     // P.V.
-    // Lane l: operand row l % 16, keys 16 (l / 16) + 8 m + 0..7, in the nibbles' order
-    // 0 4 1 5 2 6 3 7 (GP = 4: weight rows 8 to 15 repeat 0 to 7).
+    // Lane l: operand row l % 16 (digit row % 4 of head row / 4), keys 16 (l / 16) + 0..15
+    // in the nibbles' order.
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
       if (g >= ng) break;
-      const v2i nib[2] = {read_tr4(b_src[g]), read_tr4(b_src[g] + 8)};
+      const v4i B[2] = {nibbles_i8(read_tr4(b_src[g])), nibbles_i8(read_tr4(b_src[g] + 8))};
 #pragma unroll
-      for (int m = 0; m < 2; ++m) {
-        const _Float16* src = a_src + (g * 64 + 8 * m) * 2 * GP;
-        const v4s lo = read_tr16(src), hi = read_tr16(src + 2 * 2 * GP);
-        const f16x8 A = __builtin_bit_cast(f16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+      for (int n = 0; n < NS; ++n) {
+        const v2i lo = read_tr8(a_src[0] + g * 64 * GP + 4 * n), hi = read_tr8(a_src[1] + g * 64 * GP + 4 * n);
+        const v4i A = {lo.x, lo.y, hi.x, hi.y};
 #pragma unroll
-        for (int tt = 0; tt < 2; ++tt) {
-          floatx4 c = acc[2 * g + tt];
-          c = __builtin_amdgcn_mfma_f32_16x16x32_f16(A, nibbles_f16(nib[tt][m]), c, 0, 0, 0);
-          acc[2 * g + tt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(A, __builtin_bit_cast(f16x8, minus8), c, 0, 0, 0);
-        }
+        for (int tt = 0; tt < 2; ++tt)
+          acc[n][2 * g + tt] = __builtin_amdgcn_mfma_i32_16x16x64_i8(A, B[tt], acc[n][2 * g + tt], 0, 0, 0);
       }
     }
     __builtin_amdgcn_wave_barrier();
@@ -415,20 +415,19 @@ void sfa_decode_q4_kernel(DecParams p, int dd, const uint16_t* vscale) {
     page = page_next;
   }
 
-  // Both pieces' sums to LDS, with the powers of two of weights and numbers taken out
-  // (2^(137 - vexp) 2^-24).  Lane l, register i: row 4 (l / 16) + i, coordinate l % 16.
+  // The sums to LDS, with the powers of two of weights and numbers taken out (2^(155 -
+  // vexp) and 16).  Lane l, register i: digit i of head l / 16, coordinate l % 16.
 #pragma unroll
   for (int h = 0; h < GP; ++h) l_lane[h] = wave_sum_dpp(l_lane[h]);
   __syncthreads();  // every wavefront is done with pb
-  float* red_o = (float*)&pb[0][0][0][0];  // [wave][2 GP][D]
-  static_assert(sizeof(pb) >= sizeof(float) * kDecWaves * 2 * GP * D, "the partials fit the weights' place");
-  if (GP == 8 || lane < 32) {
-    float* dst = red_o + (wave * 2 * GP + 4 * (lane >> 4)) * D + (lane & 15);
+  float* red_o = (float*)&pb[0][0][0][0];  // [wave][GP][D]
+  static_assert(sizeof(pb) >= sizeof(float) * kDecWaves * GP * D, "the partials fit the weights' place");
+#pragma unroll
+  for (int n = 0; n < NS; ++n)
 #pragma unroll
     for (int t = 0; t < 2 * NG; ++t)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) dst[i * D + 16 * t] = ldexpf(acc[t][i], vexp[t / 2] - 113);
-  }
+      red_o[(wave * GP + 4 * n + (lane >> 4)) * D + (lane & 15) + 16 * t] =
+          vexp[t / 2] == 255 ? NAN : ldexpf(from_digits(acc[n][t]), vexp[t / 2] - 159);
   if (lane == 0) {
 #pragma unroll
     for (int h = 0; h < GP; ++h) { red_m[wave][h] = m_run[h]; red_l[wave][h] = l_lane[h]; }
@@ -445,7 +444,7 @@ void sfa_decode_q4_kernel(DecParams p, int dd, const uint16_t* vscale) {
     for (int w = 0; w < kDecWaves; ++w) {
       const float sc = __builtin_amdgcn_exp2f(red_m[w][h] - Mu);
       lsum += sc * red_l[w][h];
-      osum += sc * (red_o[(w * 2 * GP + h) * D + c] + red_o[(w * 2 * GP + GP + h) * D + c]);
+      osum += sc * red_o[(w * GP + h) * D + c];
     }
     const int64_t part = ((int64_t)b * p.Hq + hkv * p.G + h) * p.nch + slot;
     p.ws_o[part * d + c] = osum;
@@ -526,14 +525,14 @@ __global__ __launch_bounds__(WIDE ? 64 * kMergeQ4 : 256) void sfa_decode_q4_comb
     float sum = os[0][i];
 #pragma unroll
     for (int g = 1; g < kMergeQ4; ++g) sum += WIDE ? part[g][lane + 64 * i] : os[WIDE ? 0 : g][i];
-    const float out = lsum > 0.f ? sum / lsum : 0.f;
+    const float out = lsum == 0.f ? 0.f : sum / lsum;
     const int c = lane + 64 * i;
     if (c < d) {
       if (obf16) ((uint16_t*)o)[(int64_t)bh * d + c] = (uint16_t)f32_to_bf16_rne(out);
       else ((float*)o)[(int64_t)bh * d + c] = out;
     }
   }
-  if (lse && lane == 0) lse[bh] = lsum > 0.f ? (M + __log2f(lsum)) * kLn2 : -INFINITY;
+  if (lse && lane == 0) lse[bh] = lsum == 0.f ? -INFINITY : (M + __log2f(lsum)) * kLn2;
 }
 
 template <int NV>

@@ -165,10 +165,11 @@ def _bounds(qv, kv, vv, scale, k, L):
     """Derived bounds on O (absolute, per KV head's largest |v|) and LSE.
     A base-2 exponent t = scale log2(e) ks sum of k products is off by at most (k + 4)
     2^-24 times A = |scale| log2(e) k max|q| max|k| (a bound on the sum of its
-    magnitudes), v_exp_f32 by 2^-22 relative, two pieces of a weight by 2^-22, so a
-    weight is off by w = ln 2 * dt + 2^-21 relative; O's numerator and denominator each carry
-    that, and sums of n terms in float32 another (log-like trees and chains of at most 32
-    matrix steps and 64 merges) 128 * 2^-24."""
+    magnitudes), v_exp_f32 by 2^-22 relative, and a weight's rounding to a whole number by
+    2^-29 of the largest weight, which is more of a small one: taken as 2^-22 relative,
+    so a weight is off by w = ln 2 * dt + 2^-21 relative; O's numerator and denominator each
+    carry that, and sums of n terms in float32 another (trees and chains of at most 64
+    merges) 128 * 2^-24."""
     A = abs(scale) * 1.4427 * k * np.abs(qv).max() * np.abs(kv).max()
     w = math.log(2) * (k + 4) * 2.0 ** -24 * A + 2.0 ** -21
     return (2 * w + 256 * 2.0 ** -24), w + 64 * 2.0 ** -24
@@ -236,9 +237,44 @@ def test_decode_q4_window():
     _decode(3, 1, 4, 3000, 128, 16, 16, [2900, 2, 500], window=100, n_global=400)
 
 
+@pytest.mark.parametrize("d,G,L", [(64, 4, 64), (64, 8, 50), (128, 4, 64), (128, 2, 200), (96, 3, 33), (256, 8, 64),
+                                   (64, 4, 4096), (128, 8, 4000)])
+def test_decode_q4_products_keep_float32_accuracy(d, G, L):
+    """Weights of very different sizes times the cached numbers, element by element
+    against the sum of the magnitudes of its terms, S = sum p |v|.  Queries of one
+    coordinate, so that a base-2 exponent is one product and off by at most 5 * 2^-24 times
+    A, the largest of them (the key's scale, the query, the score's scale, the difference
+    with the maximum), and a weight by w = ln 2 * that + 2^-22 (v_exp_f32) relative; the
+    output carries a weight's error twice (numerator and sum), and at most 20 roundings of
+    2^-24 in sums and joins; a weight's rounding to a whole number is 2^-29 of the largest
+    p times the largest scale, 7 of which are at most max |v|.  Over many keys the
+    errors of single weights are as unlike as the numbers they multiply: both the output and
+    its error grow as the root of their number, and the 2-norms are in a ratio of w at most;
+    2 w is asked for."""
+    k, Hkv, B, seed = 16, 2, 2, 77
+    cache, _, ci, kv, vv = _filled(B, Hkv, L, d, k, 0, seed, None)
+    q = si.normal((B, Hkv * G, d), seed, "q", device=DEV)
+    qi, qv = sfa.sfa_topk_encode(q, k)
+    qv[..., 0], qv[..., 1:] = 3.0, 0.0
+    scale = 1.0
+    o, _ = sfa.sfa_attn_decode_q4(*cache, q_idx=qi, q_val=qv, o_dtype=torch.float32, scale=scale)
+    for b in range(B):
+        args = [x.cpu().numpy()[b:b + 1] for x in (qi, qv)] + [ci[b:b + 1], kv[b:b + 1]]
+        O, _ = oracle.attn_decode(*args, vv[b:b + 1], d, scale)
+        S, _ = oracle.attn_decode(*args, np.abs(vv[b:b + 1]), d, scale)
+        A = 1.4427 * scale * 3.0 * 2 * np.abs(kv[b]).max()
+        w = math.log(2) * 5 * 2.0 ** -24 * A + 2.0 ** -22
+        vmax = np.abs(vv[b]).reshape(Hkv, -1, d // 32, 32).max((1, 3))
+        bound = (2 * w + 20 * 2.0 ** -24) * S[0] + 2.0 ** -29 * L / 7 * np.repeat(np.repeat(vmax, 32, -1), G, 0)
+        err = np.abs(np_f64(o[b]) - O[0])
+        assert (err <= bound).all(), (b, float((err / bound).max()))
+        ratio = np.linalg.norm(err) / np.linalg.norm(O)
+        assert L < 1000 or ratio <= 2 * w, (b, ratio, w)
+
+
 def test_decode_q4_scales_of_any_size():
-    """Runs of a value row, and rows, of magnitudes from 2^-120 to 2^120: float16 weights
-    keep float32 accuracy of each run.  Large scores and both signs of the scale."""
+    """Runs of a value row, and rows, of magnitudes from 2^-120 to 2^120: the weights keep
+    float32 accuracy of each run.  Large scores and both signs of the scale."""
     mul = torch.ones((1, 1, 200, 128), device=DEV)
     mul[..., :32] = 2.0 ** 100
     mul[..., 32:64] = 1e4
@@ -251,6 +287,30 @@ def test_decode_q4_scales_of_any_size():
     _decode(1, 1, 4, 300, 128, 16, 0, [300], vmul=grow.flip(2))
     _decode(2, 1, 4, 900, 128, 16, 64, [900, 3], qmul=20.0)
     _decode(2, 1, 4, 900, 128, 16, 64, [900, 3], scale=-2.0, qmul=3.0)
+
+
+def test_decode_q4_infinite_scales():
+    """An infinite or NaN scale of a value run reaches its coordinates of the keys that are
+    seen, and no others; of a key that is not seen, nothing.  A code scale that is NaN
+    makes the head's output NaN."""
+    B, Hkv, L, d, k, G = 2, 1, 200, 128, 16, 4
+    cache, _, _, _, _ = _filled(B, Hkv, L, d, k, 0, 11, None)
+    q = si.normal((B, G, d), 11, "q", device=DEV)
+    lens = torch.tensor([150, 199], dtype=torch.int32, device=DEV)
+    want = sfa.sfa_attn_decode_q4(*cache, seq_len=lens, q=q, o_dtype=torch.float32)
+    bad = [x.clone() for x in cache]
+    bad[4][0, 0, 150:] = float("inf")   # behind the sequence
+    bad[2][0, 0, 150:] = float("nan")
+    bad[4][1, 0, 70, 1] = float("inf")
+    bad[4][1, 0, 3, 3] = float("nan")
+    o, lse = sfa.sfa_attn_decode_q4(*bad, seq_len=lens, q=q, o_dtype=torch.float32)
+    assert torch.equal(o[0], want[0][0]) and torch.equal(lse, want[1])
+    nan = o[1].isnan().view(G, 4, 32)
+    assert bool(nan[:, 1].all() and nan[:, 3].all()) and not bool(nan[:, 0].any() or nan[:, 2].any())
+    assert torch.equal(o[1].view(G, 4, 32)[:, ::2], want[0][1].view(G, 4, 32)[:, ::2])
+    bad[2][1, 0, 9] = float("nan")
+    o, lse = sfa.sfa_attn_decode_q4(*bad, seq_len=lens, q=q, o_dtype=torch.float32)
+    assert bool(o[1].isnan().all() and lse[1].isnan().all()) and torch.equal(o[0], want[0][0])
 
 
 def test_decode_q4_is_the_same_paged_and_contiguous_and_repeatable():
