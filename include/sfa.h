@@ -701,7 +701,7 @@ sfa_status sfa_kv_append_q4(const void* k_new, const void* v_new, const int64_t*
 /*
  * Decode step over a 4-bit cache: sfa_attn_decode_q8 with key j's code values
  * q_ju * ks_j and value coordinates q_jc * vs_j,c/32.  Scores and softmax in float32;
- * in P.V each weight p_j * vs_j,c/32 is rounded to a whole number of 2^-29 of the
+ * in P.V each weight p_j * vs_j,c/32 is rounded to a whole number of 2^-28 of the
  * largest p and value scale of its 32 coordinates so far (float32's own rounding where
  * that is coarser), and its products with the integers q are summed exactly.  An infinite
  * or NaN value scale of a key that the query sees makes its 32 coordinates NaN.

@@ -15,7 +15,7 @@
 //            four digits' sums of one head.  The other operand is the cached nibbles as
 //            they are, at the high end of a byte: 16 q.  Products and sums are exact
 //            (1024 keys at most to a wavefront, 2^24); what is lost is the weights'
-//            rounding alone, 2^-29 of the largest p times the group's largest value scale.
+//            rounding alone, 2^-28 of the largest p times the group's largest value scale.
 // Both operands have 16 keys of one row in a lane, and both are held key by key: the
 // transposing LDS reads turn them, ds_read_b64_tr_b4 the cached nibbles and
 // ds_read_b64_tr_b8 the weights.  Value rows are loaded a block of
@@ -124,12 +124,13 @@ void sfa_decode_q4_kernel(DecParams p, int dd, const uint16_t* vscale) {
   v4i acc[NS][2 * NG];
 #pragma unroll
   for (int t = 0; t < NS * 2 * NG; ++t) acc[t / (2 * NG)][t % (2 * NG)] = v4i{0, 0, 0, 0};
-  // Per group, the exponent field of the largest value scale seen, at least 1 (255: an
-  // infinity or NaN).  Weights carry 2^(155 - vexp): p = 1 with a scale of that field
+  // Per group, an exponent field that no value scale seen so far passes (255: an
+  // infinity or NaN); raised to one more than the scale that passes it, so that a second
+  // raise is rare.  Weights carry 2^(155 - vexp): p = 1 with a scale of that field
   // becomes 2^28 to 2^29, and the largest weight is less than 2^30.9.
   int vexp[NG];
 #pragma unroll
-  for (int g = 0; g < NG; ++g) vexp[g] = 1;
+  for (int g = 0; g < NG; ++g) vexp[g] = 0;
   float pass = -INFINITY;  // exponents past it raise the maxima: 2^1.9 once there are any
 
   const int64_t kv_row0 = ((int64_t)b * p.Hkv + hkv) * p.Lmax;
@@ -353,16 +354,18 @@ void sfa_decode_q4_kernel(DecParams p, int dd, const uint16_t* vscale) {
         pass = m_run[0] == -INFINITY ? -INFINITY : 1.9f;
 #pragma unroll
         for (int n = 0; n < NS; ++n) {  // this lane's head of the four
-          const float lo = lane & 16 ? alpha[4 * n + 1] : alpha[4 * n];
-          const float hi = lane & 16 ? alpha[4 * n + 3] : alpha[4 * n + 2];
-          fa[n] = lane & 32 ? hi : lo;
+          fa[n] = alpha[4 * n];
+#pragma unroll
+          for (int h = 1; h < 4; ++h) fa[n] = lane >> 4 == h ? alpha[4 * n + h] : fa[n];
         }
       }
 #pragma unroll
       for (int g = 0; g < NG; ++g) {
-        const int vnew = max(vexp[g], (int)(wave_umax(vs[g] & 0x7fffffffu) >> 23));
+        const int vmax = (int)(wave_umax(vs[g] & 0x7fffffffu) >> 23);
+        const int vnew = vmax <= vexp[g] ? vexp[g] : vmax == 255 ? 255 : min(vmax + 1, 254);
         const float f = vnew - vexp[g] > 126 ? 0.f : pow2_field(127 + vexp[g] - vnew);
         vexp[g] = vnew;
+        if (sb == w0) continue;  // the sums are still zero
 #pragma unroll
         for (int t = 0; t < NS * 2; ++t) {  // rounded to 24 bits, kept as two digits
           v4i& a = acc[t / 2][2 * g + t % 2];

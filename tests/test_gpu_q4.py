@@ -166,7 +166,7 @@ def _bounds(qv, kv, vv, scale, k, L):
     A base-2 exponent t = scale log2(e) ks sum of k products is off by at most (k + 4)
     2^-24 times A = |scale| log2(e) k max|q| max|k| (a bound on the sum of its
     magnitudes), v_exp_f32 by 2^-22 relative, and a weight's rounding to a whole number by
-    2^-29 of the largest weight, which is more of a small one: taken as 2^-22 relative,
+    2^-28 of the largest weight, which is more of a small one: taken as 2^-22 relative,
     so a weight is off by w = ln 2 * dt + 2^-21 relative; O's numerator and denominator each
     carry that, and sums of n terms in float32 another (trees and chains of at most 64
     merges) 128 * 2^-24."""
@@ -246,7 +246,7 @@ def test_decode_q4_products_keep_float32_accuracy(d, G, L):
     A, the largest of them (the key's scale, the query, the score's scale, the difference
     with the maximum), and a weight by w = ln 2 * that + 2^-22 (v_exp_f32) relative; the
     output carries a weight's error twice (numerator and sum), and at most 20 roundings of
-    2^-24 in sums and joins; a weight's rounding to a whole number is 2^-29 of the largest
+    2^-24 in sums and joins; a weight's rounding to a whole number is 2^-28 of the largest
     p times the largest scale, 7 of which are at most max |v|.  Over many keys the
     errors of single weights are as unlike as the numbers they multiply: both the output and
     its error grow as the root of their number, and the 2-norms are in a ratio of w at most;
@@ -265,7 +265,7 @@ def test_decode_q4_products_keep_float32_accuracy(d, G, L):
         A = 1.4427 * scale * 3.0 * 2 * np.abs(kv[b]).max()
         w = math.log(2) * 5 * 2.0 ** -24 * A + 2.0 ** -22
         vmax = np.abs(vv[b]).reshape(Hkv, -1, d // 32, 32).max((1, 3))
-        bound = (2 * w + 20 * 2.0 ** -24) * S[0] + 2.0 ** -29 * L / 7 * np.repeat(np.repeat(vmax, 32, -1), G, 0)
+        bound = (2 * w + 20 * 2.0 ** -24) * S[0] + 2.0 ** -28 * L / 7 * np.repeat(np.repeat(vmax, 32, -1), G, 0)
         err = np.abs(np_f64(o[b]) - O[0])
         assert (err <= bound).all(), (b, float((err / bound).max()))
         ratio = np.linalg.norm(err) / np.linalg.norm(O)
