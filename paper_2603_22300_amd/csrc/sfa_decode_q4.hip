@@ -72,19 +72,20 @@ __device__ __forceinline__ float wave_sum_dpp(float x) {
   return (row(0) + row(16)) + (row(32) + row(48));
 }
 
-// D: head dimension, or 256 for any d <= 256 (dd then counts).  GP: query heads
+// D: head dimension, or with ANY at least that (dd then counts).  GP: query heads
 // per KV head rounded up to 4 or 8.  KC8: k / 8, or 0 to take it from p.k.
 // PG: 0 contiguous, 1 pages of 64 positions or more (a block of keys has one), 2
 // pages of 16 or 32.
-template <int D, int GP, int KC8, int PG>
-__global__ __launch_bounds__(kDecThreads, GP == 4 && D <= 128 ? 4 : GP == 8 && D <= 128 ? 2 : 1)
+template <int D, bool ANY, int GP, int KC8, int PG>
+__global__ __launch_bounds__(kDecThreads, GP == 4 && D <= 128 ? 4 : 2)
 void sfa_decode_q4_kernel(DecParams p, int dd, const uint16_t* vscale) {
   constexpr int NG = D / 32;  // value scale groups, two 16-coordinate tiles each
-  const int d = D == 256 ? dd : D, ng = d / 32;
+  constexpr int NP = NG < 4 || GP == 4 && D <= 128 ? NG : D / 64;  // groups whose weights are in LDS at once
+  const int d = ANY ? dd : D, ng = d / 32;
   const int k = KC8 > 0 ? 8 * KC8 : p.k;
   __shared__ float qd[256][GP];  // (an index past d reads zeros)
   __shared__ __attribute__((aligned(16))) unsigned char vt[kDecWaves][64 * D / 2];
-  __shared__ __attribute__((aligned(16))) uint32_t pb[kDecWaves][NG][64][GP];  // digits of the weights
+  __shared__ __attribute__((aligned(16))) uint32_t pb[kDecWaves][NP][64][GP];  // digits of the weights
   __shared__ float red_m[kDecWaves][GP], red_l[kDecWaves][GP];
 
   const int tid = threadIdx.x, lane = tid & 63;
@@ -175,10 +176,11 @@ void sfa_decode_q4_kernel(DecParams p, int dd, const uint16_t* vscale) {
   auto load_values = [&](int sb, int page) {  // page: of this lane's key (PG 2)
     const int last = w1 - 1 - sb;
     const uint8_t* base = PG < 2 ? vc + block_row(sb) * (d / 2) : nullptr;
-    if constexpr (PG < 2 && D <= 128) {
+    if constexpr (PG < 2 && !ANY) {
       if (last >= 63) {  // a whole block: its rows are one run
 #pragma unroll
-        for (int i = 0; i < NG; ++i) vreg[i] = *(const u32x4*)(base + run_off + i * 1024);
+        for (int i = 0; i < NG; ++i)  // (the exchange repeats after 16 keys: 8 pieces, two loads)
+          vreg[i] = *(const u32x4*)(base + (NG == 8 && i % 2 ? run_off ^ 64 : run_off) + i * 1024);
         return;
       }
     }
@@ -196,7 +198,7 @@ void sfa_decode_q4_kernel(DecParams p, int dd, const uint16_t* vscale) {
   // A key's codes and scales (lane = key), loaded a block ahead.
   constexpr int NKC = KC8 > 0 ? KC8 : 1;
   uint2 ki[NKC];
-  constexpr int NVS = D <= 128 ? NG / 2 : NG;  // value scales, two to a word where a row has 2 or 4
+  constexpr int NVS = !ANY && NG % 2 == 0 ? NG / 2 : NG;  // value scales, two to a word where a row is whole words
   uint32_t kq[NKC], vraw[NVS];
   float ks = 0.f;
   auto lane_row = [&](int sb, int page) -> int64_t {
@@ -217,10 +219,14 @@ void sfa_decode_q4_kernel(DecParams p, int dd, const uint16_t* vscale) {
     }
     ks = (p.kc_scale + row)[o];
     const uint16_t* pv = vscale + row * ng + o * ng;
-    if constexpr (D == 128) {
+    if constexpr (!ANY && D == 256) {
+      const u32x4 w = *(const u32x4*)pv;
+#pragma unroll
+      for (int g = 0; g < 4; ++g) vraw[g] = w[g];
+    } else if constexpr (!ANY && D == 128) {
       const uint2 w = *(const uint2*)pv;
       vraw[0] = w.x; vraw[1] = w.y;
-    } else if constexpr (D == 64) {
+    } else if constexpr (!ANY && D == 64) {
       vraw[0] = *(const uint32_t*)pv;
     } else {
 #pragma unroll
@@ -317,7 +323,7 @@ void sfa_decode_q4_kernel(DecParams p, int dd, const uint16_t* vscale) {
     uint32_t vs[NG];  // the value scales, as float32 bits
 #pragma unroll
     for (int g = 0; g < NG; ++g)
-      vs[g] = D > 128 ? vraw[g % NVS] << 16 : (g & 1) ? vraw[g / 2] & 0xffff0000u : vraw[g / 2] << 16;
+      vs[g] = NVS == NG ? vraw[g % NVS] << 16 : (g & 1) ? vraw[g / 2] & 0xffff0000u : vraw[g / 2] << 16;
     load_codes(sb_next, page_next);
     float t[GP];
 #pragma unroll
@@ -381,40 +387,44 @@ void sfa_decode_q4_kernel(DecParams p, int dd, const uint16_t* vscale) {
       pj[h] = __builtin_amdgcn_exp2f(t[h]);
       l_lane[h] += pj[h];
     }
-    // weights, rounded to the nearest whole number
 #pragma unroll
-    for (int g = 0; g < NG; ++g) {
-      if (g >= ng) break;
-      const float f = __builtin_ldexpf(__uint_as_float(vs[g]), 155 - vexp[g]);
+    for (int g0 = 0; g0 < NG; g0 += NP) {
+      if (g0 >= ng) break;
+      // weights, rounded to the nearest whole number
 #pragma unroll
-      for (int n = 0; n < NS; ++n) {
-        u32x4 w;
+      for (int g = g0; g < g0 + NP && g < NG; ++g) {
+        if (g >= ng) break;
+        const float f = __builtin_ldexpf(__uint_as_float(vs[g]), 155 - vexp[g]);
 #pragma unroll
-        for (int h = 0; h < 4; ++h) w[h] = digits((int)fmaf(pj[4 * n + h], f, 0.5f));
-        *(u32x4*)&pb[wave][g][place(lane)][4 * n] = w;
+        for (int n = 0; n < NS; ++n) {
+          u32x4 w;
+#pragma unroll
+          for (int h = 0; h < 4; ++h) w[h] = digits((int)fmaf(pj[4 * n + h], f, 0.5f));
+          *(u32x4*)&pb[wave][g - g0][place(lane)][4 * n] = w;
+        }
       }
-    }
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_sched_barrier(0);
-    // P.V.
-    // Lane l: operand row l % 16 (digit row % 4 of head row / 4), keys 16 (l / 16) + 0..15
-    // in the nibbles' order.
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_sched_barrier(0);
+      // P.V.
+      // Lane l: operand row l % 16 (digit row % 4 of head row / 4), keys 16 (l / 16) + 0..15
+      // in the nibbles' order.
 #pragma unroll
-    for (int g = 0; g < NG; ++g) {
-      if (g >= ng) break;
-      const v4i B[2] = {nibbles_i8(read_tr4(b_src[g])), nibbles_i8(read_tr4(b_src[g] + 8))};
+      for (int g = g0; g < g0 + NP && g < NG; ++g) {
+        if (g >= ng) break;
+        const v4i B[2] = {nibbles_i8(read_tr4(b_src[g])), nibbles_i8(read_tr4(b_src[g] + 8))};
 #pragma unroll
-      for (int n = 0; n < NS; ++n) {
-        const v2i lo = read_tr8(a_src[0] + g * 64 * GP + 4 * n), hi = read_tr8(a_src[1] + g * 64 * GP + 4 * n);
-        const v4i A = {lo.x, lo.y, hi.x, hi.y};
+        for (int n = 0; n < NS; ++n) {
+          const v2i lo = read_tr8(a_src[0] + (g - g0) * 64 * GP + 4 * n), hi = read_tr8(a_src[1] + (g - g0) * 64 * GP + 4 * n);
+          const v4i A = {lo.x, lo.y, hi.x, hi.y};
 #pragma unroll
-        for (int tt = 0; tt < 2; ++tt)
-          acc[n][2 * g + tt] = __builtin_amdgcn_mfma_i32_16x16x64_i8(A, B[tt], acc[n][2 * g + tt], 0, 0, 0);
+          for (int tt = 0; tt < 2; ++tt)
+            acc[n][2 * g + tt] = __builtin_amdgcn_mfma_i32_16x16x64_i8(A, B[tt], acc[n][2 * g + tt], 0, 0, 0);
+        }
       }
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     page = page_next;
   }
 
@@ -550,29 +560,29 @@ void launch_q4_combine(const DecParams& p, const DecodeArgs& a, hipStream_t stre
                        a.o, a.obf16, a.lse);
 }
 
-template <int D, int GP, int KC8>
+template <int D, bool ANY, int GP, int KC8>
 void launch_q4_t(const DecParams& p, const DecodeArgs& a, hipStream_t stream) {
   const dim3 grid = p.by_slot ? dim3(a.B * p.Hkv, p.nch) : dim3(p.nch, a.B * p.Hkv), block(kDecThreads);
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, p, a.d, a.v_scale16); };
-  if (!p.table) go(sfa_decode_q4_kernel<D, GP, KC8, 0>);
-  else if (p.log2P >= 6) go(sfa_decode_q4_kernel<D, GP, KC8, 1>);
-  else go(sfa_decode_q4_kernel<D, GP, KC8, 2>);
+  if (!p.table) go(sfa_decode_q4_kernel<D, ANY, GP, KC8, 0>);
+  else if (p.log2P >= 6) go(sfa_decode_q4_kernel<D, ANY, GP, KC8, 1>);
+  else go(sfa_decode_q4_kernel<D, ANY, GP, KC8, 2>);
 }
 
-template <int D, int GP>
+template <int D, bool ANY, int GP>
 void launch_q4_k(const DecParams& p, const DecodeArgs& a, hipStream_t stream) {
-  if constexpr (D < 256) {
-    if (a.k == 8) return launch_q4_t<D, GP, 1>(p, a, stream);
-    if (a.k == 16) return launch_q4_t<D, GP, 2>(p, a, stream);
-    if (a.k == 32) return launch_q4_t<D, GP, 4>(p, a, stream);
+  if constexpr (!ANY) {
+    if (a.k == 8) return launch_q4_t<D, ANY, GP, 1>(p, a, stream);
+    if (a.k == 16) return launch_q4_t<D, ANY, GP, 2>(p, a, stream);
+    if (a.k == 32) return launch_q4_t<D, ANY, GP, 4>(p, a, stream);
   }
-  launch_q4_t<D, GP, 0>(p, a, stream);
+  launch_q4_t<D, ANY, GP, 0>(p, a, stream);
 }
 
-template <int D>
+template <int D, bool ANY = false>
 void launch_q4_g(const DecParams& p, const DecodeArgs& a, hipStream_t stream) {
-  if (p.G <= 4) launch_q4_k<D, 4>(p, a, stream);
-  else launch_q4_k<D, 8>(p, a, stream);
+  if (p.G <= 4) launch_q4_k<D, ANY, 4>(p, a, stream);
+  else launch_q4_k<D, ANY, 8>(p, a, stream);
 }
 
 }  // namespace
@@ -587,7 +597,9 @@ hipError_t launch_attn_decode_q4(const DecodeArgs& a, hipStream_t stream) {
   const DecParams p = make_dec_params(a);
   if (a.d == 64) launch_q4_g<64>(p, a, stream);
   else if (a.d == 128) launch_q4_g<128>(p, a, stream);
-  else launch_q4_g<256>(p, a, stream);
+  else if (a.d == 96) launch_q4_g<96>(p, a, stream);
+  else if (a.d == 256) launch_q4_g<256>(p, a, stream);
+  else launch_q4_g<256, true>(p, a, stream);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   if (a.d <= 64) launch_q4_combine<1>(p, a, stream);

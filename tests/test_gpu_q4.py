@@ -237,6 +237,16 @@ def test_decode_q4_window():
     _decode(3, 1, 4, 3000, 128, 16, 16, [2900, 2, 500], window=100, n_global=400)
 
 
+@pytest.mark.parametrize("P", [0, 16, 64])
+@pytest.mark.parametrize("k", [8, 16, 24, 32])
+@pytest.mark.parametrize("G", [3, 8])
+@pytest.mark.parametrize("d", [32, 64, 96, 128, 192, 256])
+def test_decode_q4_forms(d, G, k, P):
+    """Every head dimension, group, code count and paging has a kernel of its own: whole
+    blocks of keys, a last one of one key or some, and a sequence of one key."""
+    _decode(3, 1, G, 387, d, k, P, [387, 321, 1], dense=G == 3)
+
+
 @pytest.mark.parametrize("d,G,L", [(64, 4, 64), (64, 8, 50), (128, 4, 64), (128, 2, 200), (96, 3, 33), (256, 8, 64),
                                    (64, 4, 4096), (128, 8, 4000)])
 def test_decode_q4_products_keep_float32_accuracy(d, G, L):
