@@ -271,7 +271,8 @@ hipError_t launch_kv_append_q4(AppendQ4Args a, hipStream_t stream) {
   if (need > 0) {
     // eight rows a wavefront where they fill the chip eight times over, the rest left to
     // the dispatcher (see launch_rope_encode)
-    const int64_t filled = need < 2048 ? need : 2048, blocks = (need + 7) / 8 > filled ? (need + 7) / 8 : filled;
+    const int64_t filled = need < 2048 ? need : 2048, most = (need + 7) / 8 > filled ? (need + 7) / 8 : filled;
+    const int64_t blocks = most < 1 << 22 ? most : 1 << 22;  // (a grid dimension: less than 2^32 threads)
     const dim3 grid((unsigned)blocks);
     a.log2P = -1;
     if ((a.page_size & (a.page_size - 1)) == 0)

@@ -133,8 +133,8 @@ __device__ __forceinline__ void fill(const PageArgs& a, int b, int me, int lanes
   const int rel0 = ws.rel0[b], need0 = ws.need0[b], row0 = ws.row0[b];
   int32_t* row = a.table + (int64_t)b * a.max_pages;
   for (int j = me; j < s.rel; j += lanes) {
-    const int p = F + rel0 + j;
-    if (p < left) a.free_pages[p] = row[s.want + j];
+    const uint32_t p = (uint32_t)F + (uint32_t)(rel0 + j);  // (may pass 2^31 where lengths and list disagree)
+    if (p < (uint32_t)left) a.free_pages[p] = row[s.want + j];
   }
   const int grant = min(max(S - need0, 0), s.need);
   for (int j = me; j < grant; j += lanes) row[s.have + j] = stack_page(a, all_rel0, F, S - 1 - need0 - j);

@@ -153,6 +153,9 @@ __device__ __forceinline__ void unit_rotate(bool neighbours, const float (&c)[VP
   for (int i = 0; i < VP; ++i) { a[i] = r[i]; b[i] = r[VP + i]; }
 }
 
+// The workgroup's place in a grid of token blocks (block_grid).
+__device__ __forceinline__ uint32_t block_of() { return blockIdx.z * gridDim.x + blockIdx.x; }
+
 // A workgroup takes a run of tokens, one lane per unit of a token's row, and all
 // heads of its slice (grid y) with the lane's cosines and sines in registers.
 // Bound by memory: 16-byte accesses (VP = 4) where rot, d, strides and addresses
@@ -160,7 +163,7 @@ __device__ __forceinline__ void unit_rotate(bool neighbours, const float (&c)[VP
 template <int VP, typename XT, typename YT>
 __global__ __launch_bounds__(256) void sfa_rope_kernel(RopePlan pl, RopeArgs a) {
   const int U = a.units, r = threadIdx.x / U, u = threadIdx.x - r * U;
-  const uint32_t tok = blockIdx.x * (uint32_t)(256 / U) + r;  // (B * n < 2^31)
+  const uint32_t tok = block_of() * (uint32_t)(256 / U) + r;  // (B * n < 2^31, and the last block near it)
   if (r >= 256 / U || tok >= (uint32_t)(a.B * a.n)) return;
   const uint32_t b = a.B == 1 ? 0 : tok / (uint32_t)a.n, t = tok - b * a.n;
   const Unit<VP> un(pl, u);
@@ -302,7 +305,7 @@ __global__ __launch_bounds__(256) void sfa_rope_bwd_kernel(RopePlan pl, RopeArgs
   float* rows = rows_lds + wave * (kBwdLds / 4);
   const int U = a.units, R = a.tokens, d = a.d;
   constexpr int NIT = VP == 1 ? 2 : 1;  // up to 128 units where VP = 1
-  const uint32_t ntok = (uint32_t)(a.B * a.n), tok0 = (blockIdx.x * 4 + wave) * (uint32_t)R;  // (< 2^31)
+  const uint32_t ntok = (uint32_t)(a.B * a.n), tok0 = (block_of() * 4 + wave) * (uint32_t)R;  // (as above)
   if (tok0 >= ntok) return;  // uniform per wave; no workgroup barrier below
   const int here = (int)min((uint32_t)R, ntok - tok0);
   const int h0 = blockIdx.y * a.heads, h1 = min(a.H, h0 + a.heads);
@@ -400,6 +403,13 @@ int heads_per_slice(int64_t blocks, int H, int64_t want) {
   return (int)((H + slices - 1) / slices);
 }
 
+// Token blocks by slices of the heads.  A grid dimension holds less than 2^32 threads:
+// blocks past 2^20 go to the third, in equal parts.
+dim3 block_grid(int64_t blocks, int slices) {
+  const int64_t z = (blocks + (1 << 20) - 1) >> 20;
+  return dim3((unsigned)((blocks + z - 1) / z), (unsigned)slices, (unsigned)z);
+}
+
 template <int VP>
 void launch_rope_t(const RopePlan& pl, const RopeArgs& a, dim3 grid, hipStream_t stream) {
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, pl, a); };
@@ -446,7 +456,7 @@ hipError_t launch_rope(const RopePlan& pl, RopeArgs a, hipStream_t stream) {
   const int per = 256 / a.units;
   const int64_t blocks = ((int64_t)a.B * a.n + per - 1) / per;
   a.heads = heads_per_slice(blocks, a.H, 2048);
-  const dim3 grid((unsigned)blocks, (unsigned)((a.H + a.heads - 1) / a.heads));
+  const dim3 grid = block_grid(blocks, (a.H + a.heads - 1) / a.heads);
   if (vec) launch_rope_t<4>(pl, a, grid, stream);
   else launch_rope_t<1>(pl, a, grid, stream);
   return hipGetLastError();
@@ -462,7 +472,8 @@ hipError_t launch_rope_encode(const RopePlan& pl, RopeArgs a, hipStream_t stream
   const int64_t slices = (a.H + a.heads - 1) / a.heads, need = (ntok + 3) / 4;
   const int64_t per = a.heads >= 32 ? 1 : 32 / a.heads, full = (2047 + slices) / slices;
   const int64_t filled = need < full ? need : full, blocks = (need + per - 1) / per;
-  const dim3 grid((unsigned)(blocks > filled ? blocks : filled), (unsigned)slices);
+  const int64_t most = blocks > filled ? blocks : filled;
+  const dim3 grid((unsigned)(most < 1 << 22 ? most : 1 << 22), (unsigned)slices);  // (as block_grid: 2^32 threads)
   if (a.xbf16) launch_encode_e<true>(pl, a, grid, stream);
   else launch_encode_e<false>(pl, a, grid, stream);
   return hipGetLastError();
@@ -477,7 +488,7 @@ hipError_t launch_rope_encode_bwd(const RopePlan& pl, RopeArgs a, hipStream_t st
   // at d = 64: 11.1 with three heads a slice, 14.5 with one, 15.8 with all)
   a.heads = heads_per_slice(blocks, a.H, 8192);
   if (a.heads < 3) a.heads = a.H < 3 ? a.H : 3;
-  const dim3 grid((unsigned)blocks, (unsigned)((a.H + a.heads - 1) / a.heads));
+  const dim3 grid = block_grid(blocks, (a.H + a.heads - 1) / a.heads);
   // code entries a lane holds: at most 64 k / U, k <= 8 U (VP = 4) or 2 U
   const int ne = (a.tokens * a.k + 63) / 64;
   if (vec) {

@@ -192,3 +192,31 @@ def test_rope_python_refusals():
         sfa.sfa_rope(x, pos, plan, y=x[:1])
     with pytest.raises(sfa.SfaError):
         sfa.sfa_rope_encode(x, pos, plan, 65)
+
+
+def test_rope_of_more_blocks_than_one_grid_dimension():
+    """Millions of tokens one element at a time (rows that start off any boundary of four):
+    the first, middle and last tokens are those of a call on them alone."""
+    d, n, k = 256, (1 << 22) + 5, 8
+    plan = sfa.sfa_rope_plan(d, theta=1e4)
+    x = torch.zeros((1, 1, n, d + 1), dtype=torch.bfloat16, device=DEV)[..., :d]
+    pos = torch.arange(n, dtype=torch.int32, device=DEV)
+    idx = torch.zeros((1, 1, n, k), dtype=torch.uint8, device=DEV)
+    g = torch.zeros((1, 1, n, k), device=DEV)
+    spans = [slice(0, 7), slice(1 << 21, (1 << 21) + 9), slice(n - 6, n)]
+    for i, s in enumerate(spans):
+        x[:, :, s] = torch.randn(x[:, :, s].shape, generator=torch.Generator().manual_seed(i)).to(DEV, torch.bfloat16)
+        g[:, :, s] = torch.randn(g[:, :, s].shape, generator=torch.Generator().manual_seed(9 + i)).to(DEV)
+        idx[:, :, s] = torch.arange(k, dtype=torch.uint8, device=DEV) * 31
+    y = sfa.sfa_rope(x, pos, plan)
+    ci, cv = sfa.sfa_rope_encode(x, pos, plan, k, idx_dtype=torch.uint8, val_dtype=torch.float16)
+    dx = torch.empty((1, 1, n, d + 1), dtype=torch.bfloat16, device=DEV)[..., :d]
+    sfa.sfa_rope_encode_bwd(idx, g, pos, plan, dx=dx)
+    for s in spans:
+        part = x[:, :, s].contiguous()
+        assert torch.equal(y[:, :, s], sfa.sfa_rope(part, pos[s], plan))
+        pi, pv = sfa.sfa_rope_encode(part, pos[s], plan, k, idx_dtype=torch.uint8, val_dtype=torch.float16)
+        assert torch.equal(ci[:, :, s], pi) and torch.equal(cv[:, :, s], pv)
+        pd = sfa.sfa_rope_encode_bwd(idx[:, :, s].contiguous(), g[:, :, s].contiguous(), pos[s].contiguous(), plan,
+                                     dx_dtype=torch.bfloat16)
+        assert torch.equal(dx[:, :, s], pd)
