@@ -68,8 +68,13 @@ __device__ __forceinline__ void quant4(const float (&x)[N], float s, float (&q)[
 // the division itself where the remainder could leave the normal range.
 __device__ __forceinline__ float seventh(float x) {
   const float r = 1.f / 7.f, q = x * r;
-  const float y = fmaf(fmaf(-7.f, q, x), r, q);
-  return wave_ballot(!(x >= 0x1p-90f && x < 0x1p126f)) ? x / 7.f : y;
+  float y = fmaf(fmaf(-7.f, q, x), r, q);
+  constexpr uint32_t lo = (127u - 90) << 23, hi = (127u + 126) << 23;
+  if (wave_ballot(__float_as_uint(x) - lo >= hi - lo)) {
+    asm volatile("" : "+v"(x));  // (or the division is made of every row, and then not used)
+    y = x / 7.f;
+  }
+  return y;
 }
 
 __device__ __forceinline__ int64_t clamp_len(int64_t L, int64_t cap) { return L < 0 ? 0 : (L > cap ? cap : L); }
@@ -92,7 +97,7 @@ __global__ __launch_bounds__(256) void sfa_kv_append_q4_kernel(AppendQ4Args a) {
   int t = (int)(w / a.Hkv % a.T);
   int b = (int)(w / a.Hkv / a.T);
 
-  uint32_t nk[E], nv[NV][2];
+  uint32_t nk[E], nv[NV][2];  // as loaded: what would widen them here would wait for them
   // The row's place: its slot, or its position and page, as they are loaded (nothing
   // waits for them before the row's turn).
   int nplace = 0;
@@ -110,12 +115,10 @@ __global__ __launch_bounds__(256) void sfa_kv_append_q4_kernel(AppendQ4Args a) {
     for (int i = 0; i < NV; ++i) {
       const int c = min(2 * lane + 128 * i, a.d - 2);
       if constexpr (VB && V2) {
-        const uint32_t two = *(const uint32_t*)((const uint16_t*)a.v_new + vo + c);
-        nv[i][0] = two << 16;
-        nv[i][1] = two & 0xffff0000u;
+        nv[i][0] = *(const uint32_t*)((const uint16_t*)a.v_new + vo + c);
       } else if constexpr (VB) {
-        nv[i][0] = (uint32_t)((const uint16_t*)a.v_new + vo)[c] << 16;
-        nv[i][1] = (uint32_t)((const uint16_t*)a.v_new + vo)[c + 1] << 16;
+        nv[i][0] = ((const uint16_t*)a.v_new + vo)[c];
+        nv[i][1] = ((const uint16_t*)a.v_new + vo)[c + 1];
       } else if constexpr (V2) {
         const uint2 two = *(const uint2*)((const uint32_t*)a.v_new + vo + c);
         nv[i][0] = two.x;
@@ -167,8 +170,10 @@ __global__ __launch_bounds__(256) void sfa_kv_append_q4_kernel(AppendQ4Args a) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const bool in = 2 * lane + 128 * i < a.d;
-      x[i][0] = in ? __uint_as_float(nv[i][0]) : 0.f;
-      x[i][1] = in ? __uint_as_float(nv[i][1]) : 0.f;
+      const uint32_t v0 = VB ? nv[i][0] << 16 : nv[i][0];
+      const uint32_t v1 = VB && V2 ? nv[i][0] & 0xffff0000u : VB ? nv[i][1] << 16 : nv[i][1];
+      x[i][0] = in ? __uint_as_float(v0) : 0.f;
+      x[i][1] = in ? __uint_as_float(v1) : 0.f;
     }
     h += a.step_h;
     t += a.step_t;
