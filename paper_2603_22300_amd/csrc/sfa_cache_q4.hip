@@ -204,6 +204,16 @@ __global__ __launch_bounds__(256) void sfa_kv_append_q4_kernel(AppendQ4Args a) {
       topk_select<E>(key, a.k, sel);
       int sl[E];
       topk_slots<E>(sel, sl);
+      // (the next row's words and place are waited for before the stores, as in
+      // sfa_rope_encode_kernel)
+#pragma unroll
+      for (int e = 0; e < E; ++e) asm volatile("" : "+v"(nk[e]));
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        asm volatile("" : "+v"(nv[i][0]));
+        if constexpr (!(VB && V2)) asm volatile("" : "+v"(nv[i][1]));
+      }
+      asm volatile("" : "+v"(nplace));
       // the kept values' largest magnitude is the row's: the largest key, |bits| + 1
       const float ks = seventh(__uint_as_float(wave_umax(km) - 1u));
       float kx[E], q[E];

@@ -195,8 +195,10 @@ __global__ __launch_bounds__(256) void sfa_rope_kernel(RopePlan pl, RopeArgs a) 
 // IF, VF: output formats, or -1 to read them from the arguments.
 template <int E, int IF, int VF, bool XB, bool SAME>
 __global__ __launch_bounds__(256) void sfa_rope_encode_kernel(RopePlan pl, RopeArgs a) {
+  __shared__ uint2 ent_lds[4][E <= 1 ? 64 : 64 * E];  // kept entries of R rows: bits, coordinate
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  uint2* ent = ent_lds[wave];
   const int ifmt = IF >= 0 ? IF : a.ifmt, vfmt = VF >= 0 ? VF : a.vfmt;
   const uint32_t ntok = (uint32_t)(a.B * a.n);  // (< 2^31)
   const int half = pl.rot / 2;
@@ -220,6 +222,12 @@ __global__ __launch_bounds__(256) void sfa_rope_encode_kernel(RopePlan pl, RopeA
   uint32_t tok = blockIdx.x * 4 + wave;
   if (tok >= ntok) return;  // uniform per wave
   const int h0 = blockIdx.y * a.heads, h1 = min(a.H, h0 + a.heads);
+  // Stores: as many rows (heads of one token) as have 64 entries, and at least one.  An
+  // entry's lane is then its place in a row of its own, and a store instruction is whole
+  // runs of k (stored from where they are selected, a row took two partial ones a format).
+  const int R = a.k <= 64 ? 64 / a.k : 1;
+  const int my_row = a.k <= 64 ? lane / a.k : 0;
+  const int64_t row_step = (int64_t)a.n * a.k, my_off = my_row * row_step + (lane - my_row * a.k);
   // A row's words, and a token's positions, are loaded one row ahead, past the end
   // of a token's heads too.
   uint32_t nx[E], np[SAME ? 1 : E];
@@ -254,6 +262,7 @@ __global__ __launch_bounds__(256) void sfa_rope_encode_kernel(RopePlan pl, RopeA
     }
     tok += stride;  // (no wrap: ntok and the grid's wavefronts are below 2^31)
     const bool more = tok < ntok;
+    int held = 0;
     for (int h = h0; h < h1; ++h) {
       uint32_t bits[E], key[E];
       if constexpr (SAME) {
@@ -280,10 +289,25 @@ __global__ __launch_bounds__(256) void sfa_rope_encode_kernel(RopePlan pl, RopeA
       topk_select<E>(key, a.k, sel);
       int slot[E];
       topk_slots<E>(sel, slot);
-      const int64_t o0 = o_base + (int64_t)h * a.n * a.k;
 #pragma unroll
       for (int e = 0; e < E; ++e)
-        if (sel[e] && slot[e] < a.k) store_code(a.idx, a.val, o0 + slot[e], lane + 64 * e, bits[e], ifmt, vfmt);
+        if (sel[e] && slot[e] < a.k) ent[held * a.k + slot[e]] = make_uint2(bits[e], lane + 64 * e);
+      if (++held < R && h + 1 < h1) continue;
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      const int64_t o0 = o_base + (h + 1 - held) * row_step + my_off;
+#pragma unroll
+      for (int e = 0; e < E; ++e) {  // (more than one only where k > 64)
+        const int i = lane + 64 * e;
+        if (64 * e >= held * a.k) break;
+        if (i < held * a.k) {
+          const uint2 w = ent[i];
+          store_code(a.idx, a.val, o0 + 64 * e, (int)w.y, w.x, ifmt, vfmt);
+        }
+      }
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      held = 0;
     }
     if (!more) break;
   }
