@@ -360,18 +360,17 @@ __global__ __launch_bounds__(256) void sfa_rope_bwd_kernel(RopePlan pl, RopeArgs
 
   float c[NIT][VP], s[NIT][VP];
   int row[NIT], off0[NIT], off1[NIT];
-  bool act[NIT], two[NIT], turned[NIT];
+  bool two[NIT], turned[NIT];
   int64_t yo[NIT];
 #pragma unroll
   for (int it = 0; it < NIT; ++it) {
-    const int v = lane + 64 * it;
-    row[it] = v / U;
+    const int v = min(lane + 64 * it, here * U - 1);  // lanes past the last unit repeat it: no branch around the
+    row[it] = v / U;                                   // stores, so a wait for the entries is not one for them too
     const Unit<VP> un(pl, v - row[it] * U);
-    act[it] = row[it] < here;
-    const uint32_t tok = tok0 + (act[it] ? row[it] : 0);
+    const uint32_t tok = tok0 + row[it];
     const uint32_t b = a.B == 1 ? 0 : tok / (uint32_t)a.n, t = tok - b * a.n;
-    off0[it] = un.off0; off1[it] = un.off1; two[it] = un.n1 == VP; turned[it] = un.turned;
-    unit_turns<VP>(pl, a.pos + b * a.pos_batch + t, a.pos_axis, act[it] && un.turned, un.pair, c[it], s[it]);
+    off0[it] = un.off0; off1[it] = un.off1; two[it] = VP == 4 || un.n1 == VP; turned[it] = un.turned;
+    unit_turns<VP>(pl, a.pos + b * a.pos_batch + t, a.pos_axis, un.turned, un.pair, c[it], s[it]);
     yo[it] = b * a.ys[0] + t * a.ys[2] + h0 * a.ys[1];
   }
   for (int h = h0; h < h1; ++h) {
@@ -386,7 +385,6 @@ __global__ __launch_bounds__(256) void sfa_rope_bwd_kernel(RopePlan pl, RopeArgs
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
     for (int it = 0; it < NIT; ++it) {
-      if (!act[it]) continue;
       float p[VP], q[VP];
       const float* src = rows + row[it] * d;
       load_vec<VP>(src + off0[it], p);
@@ -508,9 +506,10 @@ hipError_t launch_rope_encode_bwd(const RopePlan& pl, RopeArgs a, hipStream_t st
   a.units = units_of(pl, vec ? 4 : 1);
   a.tokens = a.units >= 64 ? 1 : 64 / a.units;
   const int64_t blocks = ((int64_t)a.B * a.n + 4 * a.tokens - 1) / (4 * a.tokens);
-  // (32 heads, 32,768 tokens: 119 us in one slice, 109 in four; 12 heads, 8 x 1024 tokens
-  // at d = 64: 11.1 with three heads a slice, 14.5 with one, 15.8 with all)
-  a.heads = heads_per_slice(blocks, a.H, 8192);
+  // (32 heads, 32,768 tokens: 89 us in one slice, 98 in four, 126 in sixteen, each with its
+  // sines again; 12 heads, 8 x 1024 tokens at d = 64: 11.0 with three heads a slice,
+  // 14.5 with one, 15.8 with all)
+  a.heads = heads_per_slice(blocks, a.H, 2048);
   if (a.heads < 3) a.heads = a.H < 3 ? a.H : 3;
   const dim3 grid = block_grid(blocks, (a.H + a.heads - 1) / a.heads);
   // code entries a lane holds: at most 64 k / U, k <= 8 U (VP = 4) or 2 U
