@@ -202,8 +202,10 @@ __global__ __launch_bounds__(256) void sfa_kv_append_q4_kernel(AppendQ4Args a) {
     const bool more = b < a.B;
     if (more) load_row();
     if (kept) {  // uniform per wave
+      const uint32_t cut = topk_cut<E>(key, a.k);
       bool sel[E];
-      topk_select<E>(key, a.k, sel);
+#pragma unroll
+      for (int e = 0; e < E; ++e) sel[e] = key[e] >= cut;
       int sl[E];
       topk_slots<E>(sel, sl);
       // (the next row's words and place are waited for before the stores, as in

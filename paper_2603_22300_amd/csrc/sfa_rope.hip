@@ -288,8 +288,10 @@ __global__ __launch_bounds__(256) void sfa_rope_encode_kernel(RopePlan pl, RopeA
       for (int e = 0; e < E; ++e) key[e] = topk_key(bits[e], lane + 64 * e < a.d);
       if (h + 1 < h1) load_row(x0 + (h + 1) * a.xs[1]);
       else if (more) open_token();
+      const uint32_t cut = topk_cut<E>(key, a.k);
       bool sel[E];
-      topk_select<E>(key, a.k, sel);
+#pragma unroll
+      for (int e = 0; e < E; ++e) sel[e] = key[e] >= cut;
       int slot[E];
       topk_slots<E>(sel, slot);
 #pragma unroll

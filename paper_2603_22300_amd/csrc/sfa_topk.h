@@ -104,6 +104,49 @@ __device__ __forceinline__ void topk_select(const uint32_t (&key)[E], int k, boo
   }
 }
 
+// The same selection as a threshold: the keys at or above the result are the k kept ones
+// (ties at it that are not kept are set to 0).  One scalar leaves the search instead of a
+// lane mask per coordinate from each of its ends, which the compiler merges by some
+// fifteen instructions a row.
+template <int E, int B>
+__device__ __forceinline__ uint32_t topk_cut_from(uint32_t (&key)[E], int k, uint32_t prefix) {
+#pragma unroll
+  for (int b = B; b >= 0; --b) {
+    const uint32_t cand = prefix | (1u << b);
+    const int cnt = topk_count_ge<E>(key, cand);
+    if (cnt >= k) prefix = cand;
+    prefix = __builtin_amdgcn_readfirstlane(prefix);
+    if (cnt == k) return prefix;
+  }
+  int gt = 0;
+#pragma unroll
+  for (int e = 0; e < E; ++e) gt += __popcll(wave_ballot(key[e] > prefix));
+  int before = 0;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const uint64_t eq = wave_ballot(key[e] == prefix);
+    const int r = before + lanes_below(eq);
+    if (key[e] == prefix && r >= k - gt) key[e] = 0u;
+    before += __popcll(eq);
+  }
+  return prefix;
+}
+template <int E>
+__device__ __forceinline__ uint32_t topk_cut(uint32_t (&key)[E], int k) {
+  uint32_t mx = key[0];
+#pragma unroll
+  for (int e = 1; e < E; ++e) mx = max(mx, key[e]);
+  uint32_t h = wave_umax(mx) >> 23;  // (as topk_select)
+  int cnt = topk_count_ge<E>(key, h << 23);
+  if (cnt < k) {
+    h = h - 1u;
+    cnt = topk_count_ge<E>(key, h << 23);
+  }
+  if (cnt == k) return h << 23;
+  if (cnt > k) return topk_cut_from<E, 22>(key, k, h << 23);
+  return topk_cut_from<E, 30>(key, k, 0u);
+}
+
 // slot[e]: output position of a kept coordinate among the kept ones in
 // ascending coordinate order (the number of kept coordinates below it).
 template <int E>
