@@ -11,7 +11,7 @@
 // appends, so the row walk has no division and a number costs a product with the
 // scale's reciprocal: only where that lands next to a half is the correctly rounded
 // quotient, which decides, computed.  2 x 8192 tokens x 8 heads at d = 128, k = 16, bf16 in,
-// with the codes and values for a forward beside the cache: 66 us (127 MB; 27 at a copy's
+// with the codes and values for a forward beside the cache: 63 us (127 MB; 27 at a copy's
 // rate), the vector and the scalar unit 73% busy.
 #include "sfa_device.h"
 #include "sfa_launch.h"

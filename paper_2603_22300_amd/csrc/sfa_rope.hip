@@ -194,8 +194,8 @@ __global__ __launch_bounds__(256) void sfa_rope_kernel(RopePlan pl, RopeArgs a) 
 // loaded beside it, unless both lie in the lane already (SAME: pairing halves,
 // rot = d = 128 or 256: coordinates l + 64 e and l + 64 (e + E/2)).
 // IF, VF: output formats, or -1 to read them from the arguments.
-// Bound by the scalar unit, 83% busy with the selection: 32 heads x 32,768 rows of 128
-// float32, k = 16: 202 us, 3.3 TB/s.
+// Bound by the scalar unit, 82% busy with the selection: 32 heads x 32,768 rows of 128
+// float32, k = 16: 192 us, 3.5 TB/s.
 template <int E, int IF, int VF, bool XB, bool SAME>
 __global__ __launch_bounds__(256) void sfa_rope_encode_kernel(RopePlan pl, RopeArgs a) {
   __shared__ uint2 ent_lds[4][E <= 1 ? 64 : 64 * E];  // kept entries of R rows: bits, coordinate
