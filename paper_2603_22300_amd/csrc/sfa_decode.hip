@@ -81,7 +81,7 @@ size_t decode_workspace_bytes_min(int B, int Hq, int Lmax, int d) {
 // sequence has at most aim + 2 chunks below kDecodeChunk keys (decode_plan; under a
 // window the global keys' last chunk and the window's first are partly filled), or
 // its whole chunks of kDecodeChunk.
-int decode_most_slots(int Lmax, int aim) {
+static int most_slots(int Lmax, int aim) {
   const int fine = Lmax / kDecodeMinChunk + (Lmax % kDecodeMinChunk != 0);
   return aim == 0 ? decode_slots(Lmax, 0) : std::min(fine, std::max(decode_slots(Lmax, 0), aim + 2));
 }
@@ -96,7 +96,7 @@ size_t decode_workspace_bytes(int B, int Hq, int Lmax, int d) {
   static_assert((size_t)3 * kDecMaxG * kDecodeTargetWindow * (128 + 2) * sizeof(float) <=
                     SFA_DECODE_NOALLOC_MAX_BYTES, "a finer cut fits the scratch");
   if (d != 64 && d != 128) return decode_workspace_bytes_min(B, Hq, Lmax, d);
-  return slot_bytes(B, Hq, decode_most_slots(Lmax, decode_chunks_aim(B, (Hq + kDecMaxG - 1) / kDecMaxG, true, 1)), d);
+  return slot_bytes(B, Hq, most_slots(Lmax, decode_chunks_aim(B, (Hq + kDecMaxG - 1) / kDecMaxG, true, 1)), d);
 }
 
 int decode_aim(int B, int Hq, int Hkv, int Lmax, int d, int window, size_t ws_bytes, bool q8) {
@@ -152,7 +152,7 @@ DecParams make_dec_params(const DecodeArgs& a) {
   if (a.window > 0 && wspan < a.Lmax) {
     // a sequence still inside the window, or whose query is a global token,
     // is cut as without one: its length is at most wspan
-    p.nch = std::min(decode_slots((int)wspan, a.aim) + 2, decode_most_slots(a.Lmax, a.aim));
+    p.nch = std::min(decode_slots((int)wspan, a.aim) + 2, most_slots(a.Lmax, a.aim));
   }
   // The 8-bit cache's step is bound by its arithmetic, and slots that a sequence does
   // not have, dispatched among the others, leave compute units with fewer workgroups: by

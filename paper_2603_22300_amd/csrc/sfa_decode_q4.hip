@@ -31,6 +31,8 @@
 // Bound by reads beside the vector unit: 64 sequences x 8 heads x 65,536 keys (d = 128, k =
 // 16, 3.36 GB) 595 us, 5.6 TB/s, the vector unit 53% and the LDS 40% busy, the matrix cores
 // 5%; one sequence of 3000 keys 10 us with its merge.
+#include <algorithm>
+
 #include "sfa_decode_kernel.h"
 
 namespace sfa {
@@ -591,10 +593,13 @@ void launch_q4_g(const DecParams& p, const DecodeArgs& a, hipStream_t stream) {
 
 }  // namespace
 
-// For any group and window, as decode_workspace_bytes, at any head dimension.
+// For any group and window, as decode_workspace_bytes, at any head dimension: a sequence has
+// at most aim + 2 chunks below kDecodeChunk keys, or its whole chunks of kDecodeChunk.
 size_t decode_q4_workspace_bytes(int B, int Hq, int Lmax, int d) {
   const int aim = decode_chunks_aim(B, (Hq + kDecMaxG - 1) / kDecMaxG, true, 1);
-  return (size_t)B * Hq * (size_t)decode_most_slots(Lmax, aim) * (size_t)(d + 2) * sizeof(float);
+  const int fine = Lmax / kDecodeMinChunk + (Lmax % kDecodeMinChunk != 0), whole = decode_slots(Lmax, 0);
+  const int slots = aim == 0 ? whole : std::min(fine, std::max(whole, aim + 2));
+  return (size_t)B * Hq * (size_t)slots * (size_t)(d + 2) * sizeof(float);
 }
 
 hipError_t launch_attn_decode_q4(const DecodeArgs& a, hipStream_t stream) {

@@ -104,8 +104,6 @@ inline int decode_slots(int span, int aim) {
   return fine < most ? fine : most;
 }
 hipError_t launch_attn_decode(const DecodeArgs& a, hipStream_t stream);
-// The most partial slots of a step over Lmax keys with that aim, windowed or not.
-int decode_most_slots(int Lmax, int aim);
 // Workspace of any step of these sizes, and of one in chunks of kDecodeChunk
 // keys (never more than the former).
 size_t decode_workspace_bytes(int B, int Hq, int Lmax, int d);
