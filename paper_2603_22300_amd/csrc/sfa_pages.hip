@@ -68,7 +68,7 @@ __device__ __forceinline__ int wave_scan(int x, int lane) {  // inclusive
 __device__ __forceinline__ void plan(const PageArgs& a, const PageWs& ws) {
   __shared__ int part[3][kPlanThreads / 64];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  int base[3] = {0, 0, 0};  // sums over the sequences before this round's
+  int base[3] = {0, 0, 0};  // sums over the sequences before these
   for (int b0 = 0; b0 < a.B; b0 += kPlanThreads) {
     const int b = b0 + tid;
     int v[3] = {0, 0, 0}, in[3];

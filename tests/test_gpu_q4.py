@@ -407,3 +407,17 @@ def test_q4_python_refusals():
     with pytest.raises(sfa.SfaError) as e:
         sfa.sfa_attn_decode_q4(*cache, q=torch.zeros((2, 18, 128), device=DEV))
     assert e.value.status == sfa.SFA_ENOTSUP
+
+
+@pytest.mark.parametrize("d,k", [(32, 8), (32, 32), (64, 16), (96, 24), (128, 16), (128, 128), (224, 40), (256, 256)])
+def test_append_q4_of_ties(d, k):
+    """Keys of one value, of zeros and of few values: the kept coordinates are
+    sfa_topk_encode's, ties to the lower one."""
+    g = torch.Generator().manual_seed(d + k)
+    rows = torch.cat([torch.zeros(5, d), torch.full((5, d), -1.5), torch.randint(-2, 3, (60, d), generator=g).float()])
+    n = rows.shape[0]
+    kn = rows.to(DEV)[None, None].contiguous()
+    cache = _cache(1, 1, n, d, k)
+    sfa.sfa_kv_append_q4(kn, kn, torch.zeros(1, dtype=torch.int32, device=DEV), *cache, k=k)
+    wi, _ = sfa.sfa_topk_encode(kn, k)
+    assert torch.equal(cache[0].int(), wi.int())

@@ -220,3 +220,25 @@ def test_rope_of_more_blocks_than_one_grid_dimension():
         pd = sfa.sfa_rope_encode_bwd(idx[:, :, s].contiguous(), g[:, :, s].contiguous(), pos[s].contiguous(), plan,
                                      dx_dtype=torch.bfloat16)
         assert torch.equal(dx[:, :, s], pd)
+
+
+@pytest.mark.parametrize("d", [2, 48, 64, 96, 128, 200, 256])
+def test_rope_encode_of_ties(d):
+    """Rows of one value, of zeros, of few values, with infinities and NaN, at k from 1 to d:
+    the code is sfa_topk_encode's of the rotated rows, ties to the lower coordinate."""
+    g = torch.Generator().manual_seed(d)
+    rows = [torch.zeros(9, d), torch.full((9, d), -1.5), torch.randint(-2, 3, (40, d), generator=g).float(),
+            torch.randint(0, 2, (20, d), generator=g).float() * 2.0 ** -140, torch.randn(30, d, generator=g)]
+    odd = torch.randn(20, d, generator=g)
+    odd[:, 0] = float("inf")
+    odd[::3, d // 2] = float("nan")
+    x = torch.cat(rows + [odd]).to(DEV)[None, None].repeat(1, 3, 1, 1).contiguous()
+    pos = torch.zeros(x.shape[2], dtype=torch.int32, device=DEV)
+    pos[::2] = 77
+    for pairing in ("halves", "neighbours"):
+        plan = sfa.sfa_rope_plan(d, theta=1e4, pairing=pairing)
+        y = sfa.sfa_rope(x, pos, plan)
+        for k in sorted({1, 2, min(d, 16), d // 2, d - 1, d}):
+            i, v = sfa.sfa_rope_encode(x, pos, plan, k)
+            wi, wv = sfa.sfa_topk_encode(y, k)
+            assert torch.equal(i, wi) and torch.equal(v.view(torch.int32), wv.view(torch.int32)), (pairing, k)
