@@ -82,8 +82,10 @@ __device__ __forceinline__ float wave_sum_dpp(float x) {
 // per KV head rounded up to 4 or 8.  KC8: k / 8, or 0 to take it from p.k.
 // PG: 0 contiguous, 1 pages of 64 positions or more (a block of keys has one), 2
 // pages of 16 or 32.
+// Wavefronts per SIMD: 8 query heads at d = 128 take two registers more than three allow;
+// held to three, 64 x 4000 keys 65.6 -> 61.9 us.
 template <int D, bool ANY, int GP, int KC8, int PG>
-__global__ __launch_bounds__(kDecThreads, GP == 4 && D <= 128 ? 4 : 2)
+__global__ __launch_bounds__(kDecThreads, GP == 4 && D <= 128 ? 4 : D <= 128 ? 3 : 2)
 void sfa_decode_q4_kernel(DecParams p, int dd, const uint16_t* vscale) {
   constexpr int NG = D / 32;  // value scale groups, two 16-coordinate tiles each
   constexpr int NP = NG < 4 || GP == 4 && D <= 128 ? NG : D / 64;  // groups whose weights are in LDS at once
