@@ -572,6 +572,8 @@ template <int D, bool ANY, int GP, int KC8>
 void launch_q4_t(const DecParams& p, const DecodeArgs& a, hipStream_t stream) {
   const dim3 grid = p.by_slot ? dim3(a.B * p.Hkv, p.nch) : dim3(p.nch, a.B * p.Hkv), block(kDecThreads);
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, p, a.d, a.v_scale16); };
+  // A block of 64 keys is one run of rows in pages of 64 and more, whose base is scalar (d =
+  // 128, 64 x 4000 keys, 8 query heads a group: 61.5 us, with an address a lane 64.5).
   if (!p.table) go(sfa_decode_q4_kernel<D, ANY, GP, KC8, 0>);
   else if (p.log2P >= 6) go(sfa_decode_q4_kernel<D, ANY, GP, KC8, 1>);
   else go(sfa_decode_q4_kernel<D, ANY, GP, KC8, 2>);
@@ -579,6 +581,9 @@ void launch_q4_t(const DecParams& p, const DecodeArgs& a, hipStream_t stream) {
 
 template <int D, bool ANY, int GP>
 void launch_q4_k(const DecParams& p, const DecodeArgs& a, hipStream_t stream) {
+  // k known: the codes of the next block are loaded while this one is multiplied (64 x 4000
+  // keys, k = 16, against codes read in their turn: d = 64 29.1 and 32.4 us, d = 128 with 8
+  // query heads a group 61.5 and 72.2, d = 256 101 and 120).
   if constexpr (!ANY) {
     if (a.k == 8) return launch_q4_t<D, ANY, GP, 1>(p, a, stream);
     if (a.k == 16) return launch_q4_t<D, ANY, GP, 2>(p, a, stream);
@@ -606,6 +611,8 @@ size_t decode_q4_workspace_bytes(int B, int Hq, int Lmax, int d) {
 
 hipError_t launch_attn_decode_q4(const DecodeArgs& a, hipStream_t stream) {
   const DecParams p = make_dec_params(a);
+  // d known: no divisions and no absent groups in the loop (64 x 4000 keys, k = 16, against the
+  // kernel of any d: d = 96 35.7 and 63.3 us, d = 256 with 8 query heads a group 101 and 202).
   if (a.d == 64) launch_q4_g<64>(p, a, stream);
   else if (a.d == 128) launch_q4_g<128>(p, a, stream);
   else if (a.d == 96) launch_q4_g<96>(p, a, stream);
